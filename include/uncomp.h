@@ -13,6 +13,14 @@
  *   uncomp_decode_init     cumulative scores of the compacted cache from the prefill score
  *   uncomp_decode_step     one token: attention over the cache, score update, eviction
  *
+ * or, with the compacted rows in pages instead of one dense block per head:
+ *
+ *   uncomp_prefill_attention  causal attention over whole prompts, with the normalisers that
+ *                          uncomp_window_score can take over
+ *   uncomp_paged_append    rows of a compacted cache join the pages of their heads
+ *   uncomp_paged_step      one token: attention over the pages, score update
+ *   uncomp_paged_evict     heads above their budget give up their lowest-scoring rows
+ *
  * and, between the layers of the prefill where the token count drops:
  *
  *   uncomp_hidden_evict    last-token attention -> top-N rows of the hidden states
@@ -39,8 +47,8 @@
  *     returns a negative status, launches nothing and leaves outputs untouched.
  *     uncomp_last_error gives a one-line reason.
  *   - Supported: D == 128, and D == 64 in the four hot calls (64-wide heads run on the plain
- *     arithmetic units, not the matrix cores: correct, several times slower; every other call
- *     takes D == 128 only); dtype bf16 or fp32; 1 <= k_trunc; pool odd, 1 <= pool <= 15;
+ *     arithmetic units, not the matrix cores: correct, several times slower), in
+ *     uncomp_prefill_attention and in the paged calls (every other call takes D == 128 only); dtype bf16 or fp32; 1 <= k_trunc; pool odd, 1 <= pool <= 15;
  *     0 < w < N; M >= 1 dividing H.  Anything else is UNCOMP_ERR_UNSUPPORTED.
  */
 #ifndef UNCOMP_H
@@ -384,6 +392,103 @@ uncomp_status uncomp_prepare_finish(uncomp_ctx* ctx, int n_layer, int H, int M,
 uncomp_status uncomp_budgets_from_labels(uncomp_ctx* ctx, const int32_t* labels, int n_layer,
                                          int n_batch, int H, int n_max, int step, int N, int w,
                                          int32_t* head_budget, void* stream);
+
+/*
+ * Causal attention over whole prompts: H KV heads with G query heads each (query head q reads KV
+ * head q / G), n_seq sequences of different lengths, packed behind one another or padded.
+ *
+ * A sequence has nq query rows, the last nq of its nk positions: query row i sees the keys
+ * j <= nk - nq + i (nk == nq is a whole prompt, nk > nq a later part of one whose earlier keys are
+ * there already).  Per query head and row, in fp32: lse = ln sum_j exp(q_i . k_j / sqrt(D)),
+ * out_i = sum_j exp(q_i . k_j / sqrt(D) - lse) v_j.  A row that sees no key (nk < nq) gives
+ * out = 0, lse = -inf.  A logit of -inf is a key without weight; +inf or NaN makes its row NaN.
+ * Keys and values that a row does not see do not touch it, whatever they are (NaN included).
+ * bf16: the weights are rounded to bf16 before they multiply the values, and the result is
+ * rounded to bf16; logits, sums and lse are fp32.
+ *
+ * Where the rows are: row r of sequence s, head h of Q is at element s*q_strides[0] +
+ * h*q_strides[1] + r*q_strides[2], features contiguous; K, V and out likewise (out is of `dtype`
+ * and has Q's heads and rows).  lse_out (floats, may be NULL): s*lse_strides[0] +
+ * h*lse_strides[1] + r.  Which rows belong to sequence s (DEVICE int32 arrays, each may be NULL):
+ *   q_first NULL: rows 0 ... q_len[s] - 1, or all q_rows without q_len            (padded)
+ *   q_first, q_len NULL: rows q_first[s] ... q_first[s + 1] - 1, n_seq + 1 entries  (packed)
+ *   both: q_len[s] rows from q_first[s] on.
+ * k_first / k_len say the same of K and V, independently of the queries.  Packed rows usually
+ * have a sequence stride of 0.  q_rows / k_rows are the rows that a sequence may address: starts
+ * and lengths are cut to them.  Rows of out / lse_out that belong to no sequence are left alone; key
+ * rows may be shared by sequences, query rows may not.
+ * Strides are multiples of 8 elements, none negative, row strides >= D; Q, K, V and out 16-byte aligned;
+ * D 64 or 128; q_rows*G <= 2^30.  Workspace: uncomp_prefill_attention_workspace_bytes.
+ */
+size_t uncomp_prefill_attention_workspace_bytes(int n_seq, int H, int G, int D, int q_rows, int k_rows);
+uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const void* K, const void* V,
+                                       uncomp_dtype dtype, int n_seq, int H, int G, int D,
+                                       int q_rows, int k_rows, const int32_t* q_first,
+                                       const int32_t* q_len, const int32_t* k_first,
+                                       const int32_t* k_len, const int64_t q_strides[3],
+                                       const int64_t k_strides[3], const int64_t v_strides[3],
+                                       void* out, const int64_t out_strides[3], float* lse_out,
+                                       const int64_t lse_strides[2], void* stream);
+
+/*
+ * Paged cache: the rows of every KV head (any mix of layers and sequences) live in pages of one
+ * pool, so that heads with different budgets hold what they need.  Row r of head h is row
+ * r % page of page table[h][r / page].  The struct is HOST memory and read during the call only;
+ * what it points to is DEVICE memory owned by the caller.  The caller hands pages out: a page
+ * belongs to one head and stands in its table once.  A table entry outside [0, n_pages) is no page;
+ * rows there are not attended to and not written.  page is 16, 32, 64, 128 or 256;
+ * max_pages*page <= 2^26; D 64 or 128; K_pages and V_pages 16-byte aligned.
+ * Workspace of the three calls: uncomp_paged_workspace_bytes, rows = max_pages*page.
+ */
+typedef struct {
+    void* K_pages;            /* [n_pages][page][D] of dtype                      */
+    void* V_pages;            /* [n_pages][page][D]                               */
+    int32_t* idx_pages;       /* [n_pages][page]: a row's original position       */
+    float* cum_pages;         /* [n_pages][page]: its cumulative score            */
+    const int32_t* table;     /* [n_heads][max_pages]: page numbers               */
+    int32_t* len;             /* [n_heads]: rows in use                           */
+    uncomp_dtype dtype;
+    int n_heads, n_pages, page, max_pages, D;
+} uncomp_paged_cache;
+size_t uncomp_paged_workspace_bytes(int n_heads, int G, int D, int rows);
+
+/*
+ * Rows of dense caches, as uncomp_select_gather and uncomp_decode_init leave them, join behind the
+ * rows of their heads.  K / V: row r of head h at element h*strides[0] + r*strides[1] (multiples of
+ * 8, row stride >= D); idx [n_heads][rows]; cum [n_heads][rows] floats or NULL (zeros); n_rows [n_heads]
+ * the rows offered per head (cut to rows), NULL: all.  A head takes as many of them as its table has
+ * room and pages for, in order: len[h] tells.
+ */
+uncomp_status uncomp_paged_append(uncomp_ctx* ctx, const uncomp_paged_cache* cache, const void* K,
+                                  const void* V, const int32_t* idx, const float* cum,
+                                  const int32_t* n_rows, int rows, const int64_t strides[2],
+                                  void* stream);
+
+/*
+ * One generated token over the pages: uncomp_decode_step without its eviction.  q [n_heads][G][D],
+ * k_new / v_new [n_heads][D] (dense, dtype as the cache), pos [n_heads] the token's position.
+ * Per head: the new token takes row len[h] with cumulative score 0 and len[h] grows by one (where
+ * the table has neither room nor a page for it, it is left out and len[h] stays); p_g = softmax over
+ * the rows of q_g . k / sqrt(D) in fp32; out[h][g][:] = sum_r p_gr v_r (floats [n_heads][G][D], may be
+ * NULL; zeros for a head without rows); the cumulative score of every row grows by sum_g p_gr.
+ * k_new, v_new and pos may be NULL together: the queries attend to the rows that are there.
+ * 1 <= G <= 16; q, k_new and v_new 16-byte aligned.
+ */
+uncomp_status uncomp_paged_step(uncomp_ctx* ctx, const uncomp_paged_cache* cache, const void* q, int G,
+                                const void* k_new, const void* v_new, const int32_t* pos, float* out,
+                                void* stream);
+
+/*
+ * Heads above their budget give up their rows of lowest cumulative score (what uncomp_decode_step does
+ * one by one).  Per head, with b = max(budget[h], w): if len[h] > b, the len[h] - b rows of lowest cum
+ * among those at positions <= pos[h] - w leave (all of them where there are fewer), equal scores by
+ * lower position, equal positions by lower row; a NaN score counts as more than any number.  The rows
+ * behind the new end that stay then move, in order, into the gaps before it, so that the pages behind
+ * it hold nothing; len[h] becomes the new end.  evicted [n_heads] (may be NULL) gets the number of rows
+ * that left.  The contents of rows behind the new end are unspecified.  w >= 0.
+ */
+uncomp_status uncomp_paged_evict(uncomp_ctx* ctx, const uncomp_paged_cache* cache, const int32_t* budget,
+                                 const int32_t* pos, int w, int32_t* evicted, void* stream);
 
 #ifdef __cplusplus
 }

@@ -46,6 +46,8 @@ Parity status of each function (what pins it lives in tests/test_oracle_*.py):
 """
 from __future__ import annotations
 
+import math
+
 import numpy as np
 
 # Flag bits (same numeric values as the C header so tests can pass one integer
@@ -447,3 +449,39 @@ def budgets_from_labels(labels: np.ndarray, B: int, n_max: int, step: int, N: in
     labels = np.asarray(labels)
     bud = np.clip(n_max - labels.astype(np.int64) * step, min(w, N), N).astype(np.int32)
     return np.repeat(bud[:, None, :], B, axis=1)
+
+
+def causal_attention(q: np.ndarray, k: np.ndarray, v: np.ndarray):
+    """One query head of one sequence: q [nq, D] are the last nq of the nk positions of k, v [nk, D].
+    Row i sees j <= nk - nq + i; logits of -inf weigh nothing.  Returns out [nq, D], lse [nq] (0 and -inf for a row that
+    sees nothing) and size [nq, D] = sum_j p_ij |v_j|, which rounding errors of the weights are relative to."""
+    nq, nk = len(q), len(k)
+    out, size, lse = np.zeros((nq, v.shape[1])), np.zeros((nq, v.shape[1])), np.full(nq, -np.inf)
+    for i in range(nq):
+        n = nk - nq + i + 1
+        if n <= 0:
+            continue
+        with np.errstate(invalid="ignore"):
+            z = k[:n] @ q[i] / math.sqrt(q.shape[1])
+        top = z.max()
+        if top == -np.inf:
+            continue
+        with np.errstate(invalid="ignore"):
+            e = np.exp(z - top)
+            lse[i] = top + np.log(e.sum())
+            out[i], size[i] = (e / e.sum()) @ v[:n], (e / e.sum()) @ np.abs(v[:n])
+    return out, lse, size
+
+
+def evict_lowest(cum: np.ndarray, idx: np.ndarray, budget: int, pos: int, w: int):
+    """Rows of one head above its budget: the lowest (cum, position, row) among positions <= pos - w leave.
+    Returns the rows in their new order: survivors behind the new end fill the gaps before it, in order."""
+    n = len(cum)
+    drop = max(0, n - max(budget, w))
+    order = sorted((r for r in range(n) if idx[r] <= pos - w),
+                   key=lambda r: (math.isnan(cum[r]), 0.0 if math.isnan(cum[r]) else cum[r], idx[r], r))
+    gone = set(order[:drop])
+    end = n - len(gone)
+    movers = iter([r for r in range(end, n) if r not in gone])
+    return [next(movers) if r in gone else r for r in range(end)]
+

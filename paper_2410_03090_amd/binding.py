@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -29,9 +30,26 @@ EXPORTS = (
     "uncomp_hidden_evict", "uncomp_hidden_workspace_bytes",
     "uncomp_matrix_entropy", "uncomp_matrix_workspace_bytes",
     "uncomp_prepare_reset", "uncomp_prepare_accumulate", "uncomp_prepare_finish", "uncomp_budgets_from_labels",
+    "uncomp_prefill_attention", "uncomp_prefill_attention_workspace_bytes",
+    "uncomp_paged_append", "uncomp_paged_step", "uncomp_paged_evict", "uncomp_paged_workspace_bytes",
 )
 
 _lib = None
+
+
+class PagedCache(NamedTuple):
+    """Rows of every KV head in pages of one pool; the tensors are updated in place by the paged calls."""
+    K: torch.Tensor          # [n_pages, page, D]
+    V: torch.Tensor          # [n_pages, page, D]
+    idx: torch.Tensor        # [n_pages, page] int32: original positions
+    cum: torch.Tensor        # [n_pages, page] float32: cumulative scores
+    table: torch.Tensor      # [n_heads, max_pages] int32: page numbers, anything outside the pool for no page
+    length: torch.Tensor     # [n_heads] int32: rows in use
+
+
+class _PagedCacheStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("K_pages", "V_pages", "idx_pages", "cum_pages", "table", "len")] + \
+               [(n, ctypes.c_int) for n in ("dtype", "n_heads", "n_pages", "page", "max_pages", "D")]
 
 
 class UncompError(RuntimeError):
@@ -110,6 +128,21 @@ def load_library() -> ctypes.CDLL:
     lib.uncomp_hidden_evict.restype = i32
     lib.uncomp_decode_workspace_bytes.argtypes = [i32, i32, i32]
     lib.uncomp_decode_workspace_bytes.restype = c.c_size_t
+    strides = c.POINTER(i64)
+    paged = c.POINTER(_PagedCacheStruct)
+    lib.uncomp_prefill_attention_workspace_bytes.argtypes = [i32] * 6
+    lib.uncomp_prefill_attention_workspace_bytes.restype = c.c_size_t
+    lib.uncomp_prefill_attention.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, strides, strides,
+                                             strides, vp, strides, vp, strides, vp]
+    lib.uncomp_prefill_attention.restype = i32
+    lib.uncomp_paged_workspace_bytes.argtypes = [i32] * 4
+    lib.uncomp_paged_workspace_bytes.restype = c.c_size_t
+    lib.uncomp_paged_append.argtypes = [vp, paged, vp, vp, vp, vp, vp, i32, strides, vp]
+    lib.uncomp_paged_append.restype = i32
+    lib.uncomp_paged_step.argtypes = [vp, paged, vp, i32, vp, vp, vp, vp, vp]
+    lib.uncomp_paged_step.restype = i32
+    lib.uncomp_paged_evict.argtypes = [vp, paged, vp, vp, i32, vp, vp]
+    lib.uncomp_paged_evict.restype = i32
     _lib = lib
     return lib
 
@@ -122,8 +155,8 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError(f"unsupported dtype {t.dtype}")
 
 
-def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+def _stream(device=None) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 def _ptr(t):
@@ -168,6 +201,15 @@ class Context:
     @staticmethod
     def hidden_workspace_bytes(B: int, H: int, G: int, N: int, w: int) -> int:
         return int(load_library().uncomp_hidden_workspace_bytes(B, H, G, N, w))
+
+    @staticmethod
+    def prefill_attention_workspace_bytes(n_seq: int, H: int, G: int, D: int, q_rows: int, k_rows: int) -> int:
+        return int(load_library().uncomp_prefill_attention_workspace_bytes(n_seq, H, G, D, q_rows, k_rows))
+
+    @staticmethod
+    def paged_workspace_bytes(n_heads: int, G: int, D: int, rows: int) -> int:
+        """rows: what a head's table has room for (max_pages * page)."""
+        return int(load_library().uncomp_paged_workspace_bytes(n_heads, G, D, rows))
 
     @staticmethod
     def matrix_workspace_bytes(N: int, D: int) -> int:
@@ -412,3 +454,111 @@ class Context:
             self.handle, X.data_ptr(), _dtype_code(X), n_mat, N, D, X.stride(0), X.stride(1), int(k_trunc), int(flags),
             int(n_iter), ent.data_ptr(), _ptr(eig), _stream()))
         return (ent, eig) if want_eig else ent
+
+    # -- attention over whole prompts ------------------------------------------------------------
+    def prefill_attention(self, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, G: int, q_first=None, k_first=None,
+                          q_len=None, k_len=None, out=None, lse=None, want_lse: bool = True):
+        """Causal attention.  Padded: Q [B, H*G, Nq, D], K / V [B, H, Nk, D]; packed: Q [H*G, T, D] with q_first [n_seq + 1],
+        K / V [H, T', D] with k_first (either may be packed alone; last dim contiguous, other strides free).  q_len / k_len [n_seq]:
+        rows of every sequence, where not all or not up to the next start.  The index tensors are int32 on the device.
+        Returns out (shape and dtype of Q) and lse, float32 [B, H*G, Nq] or [H*G, T] (None without want_lse); fresh
+        outputs are zeros (lse -inf) where no sequence has a row."""
+        def rows(t, first):
+            assert t.dim() == (3 if first is not None else 4) and t.stride(-1) == 1
+            return t.unsqueeze(0) if first is not None else t
+
+        def strides(t):
+            # a dimension of one entry has any stride
+            s = [d if n == 1 else st for d, n, st in zip((0, 0, t.shape[3]), t.shape, t.stride())]
+            return (ctypes.c_int64 * 3)(*s)
+
+        Q4, K4, V4 = rows(Q, q_first), rows(K, k_first), rows(V, k_first)
+        Hq, Nq, D = Q4.shape[1:]
+        H, Nk = K4.shape[1], K4.shape[2]
+        for t in (q_first, k_first, q_len, k_len):
+            assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.device == Q.device)
+        counts = {x for x in (None if q_first is None else q_first.numel() - (q_len is None), None if q_len is None else q_len.numel(),
+                              None if k_first is None else k_first.numel() - (k_len is None), None if k_len is None else k_len.numel(),
+                              None if q_first is not None else Q4.shape[0], None if k_first is not None else K4.shape[0]) if x is not None}
+        assert len(counts) == 1, "sequences are counted differently by the arguments"
+        n_seq = counts.pop()
+        assert Hq == H * G and K.shape == V.shape and K4.shape[3] == D and Q.dtype == K.dtype == V.dtype
+        assert Q.device == K.device == V.device and Q.device.index == self.device
+        if out is None:
+            out = torch.zeros_like(Q)
+        assert out.shape == Q.shape and out.dtype == Q.dtype and out.device == Q.device
+        if lse is None and want_lse:
+            lse = torch.full(Q.shape[:-1], float("-inf"), dtype=torch.float32, device=Q.device)
+        ls = None
+        if lse is not None:
+            assert lse.shape == Q.shape[:-1] and lse.dtype == torch.float32 and lse.stride(-1) == 1 and lse.device == Q.device
+            ls = (ctypes.c_int64 * 2)(*((0, lse.stride(0)) if q_first is not None else lse.stride()[:2]))
+        O4 = rows(out, q_first)
+        self._check(self.lib.uncomp_prefill_attention(
+            self.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), _dtype_code(Q), n_seq, H, int(G), D, Nq, Nk, _ptr(q_first), _ptr(q_len),
+            _ptr(k_first), _ptr(k_len), strides(Q4), strides(K4), strides(V4), out.data_ptr(),
+            strides(O4), _ptr(lse), ls, _stream(Q.device)))
+        return out, lse
+
+    # -- paged cache -----------------------------------------------------------------------------
+    def paged_new(self, n_heads: int, n_pages: int, page: int, max_pages: int, D: int = 128, dtype=torch.bfloat16):
+        """An empty cache: no pages handed out (the table holds -1), no rows."""
+        kw = dict(device=f"cuda:{self.device}")
+        return PagedCache(K=torch.zeros(n_pages, page, D, dtype=dtype, **kw), V=torch.zeros(n_pages, page, D, dtype=dtype, **kw),
+                          idx=torch.full((n_pages, page), -1, dtype=torch.int32, **kw), cum=torch.zeros(n_pages, page, **kw),
+                          table=torch.full((n_heads, max_pages), -1, dtype=torch.int32, **kw),
+                          length=torch.zeros(n_heads, dtype=torch.int32, **kw))
+
+    def _paged(self, c: PagedCache):
+        n_pages, page, D = c.K.shape
+        n_heads, max_pages = c.table.shape
+        assert c.V.shape == c.K.shape and c.V.dtype == c.K.dtype and c.idx.shape == c.cum.shape == (n_pages, page)
+        assert c.idx.dtype == c.table.dtype == c.length.dtype == torch.int32 and c.cum.dtype == torch.float32
+        assert c.length.shape == (n_heads,)
+        for t in c:
+            assert t.is_contiguous() and t.device.index == self.device
+        return ctypes.byref(_PagedCacheStruct(c.K.data_ptr(), c.V.data_ptr(), c.idx.data_ptr(), c.cum.data_ptr(), c.table.data_ptr(),
+                                              c.length.data_ptr(), _dtype_code(c.K), n_heads, n_pages, page, max_pages, D))
+
+    def paged_append(self, cache: PagedCache, K: torch.Tensor, V: torch.Tensor, idx: torch.Tensor, cum=None, rows=None):
+        """K / V [n_heads, cap, D] (last dim contiguous), idx [n_heads, cap] int32, cum [n_heads, cap] float32 or None (zeros), rows
+        [n_heads] int32 the rows offered of every head (None: all).  cache.length tells what was taken."""
+        n_heads, cap, D = K.shape
+        assert K.shape == V.shape and K.stride() == V.stride() and K.stride(2) == 1 and K.dtype == V.dtype == cache.K.dtype
+        assert n_heads == cache.length.numel() and D == cache.K.shape[2]
+        assert idx.shape == (n_heads, cap) and idx.dtype == torch.int32 and idx.is_contiguous()
+        assert cum is None or (cum.shape == (n_heads, cap) and cum.dtype == torch.float32 and cum.is_contiguous())
+        assert rows is None or (rows.shape == (n_heads,) and rows.dtype == torch.int32 and rows.is_contiguous())
+        for t in (K, V, idx, cum, rows):
+            assert t is None or t.device == cache.K.device
+        strides = (ctypes.c_int64 * 2)(0 if n_heads == 1 else K.stride(0), D if cap == 1 else K.stride(1))
+        self._check(self.lib.uncomp_paged_append(self.handle, self._paged(cache), K.data_ptr(), V.data_ptr(), idx.data_ptr(), _ptr(cum),
+                                                 _ptr(rows), cap, strides, _stream(K.device)))
+
+    def paged_step(self, cache: PagedCache, q: torch.Tensor, k_new=None, v_new=None, pos=None, out=None, want_out: bool = True):
+        """q [n_heads, G, D], k_new / v_new [n_heads, D], pos [n_heads] int32 (the three may be None together).  Returns out
+        [n_heads, G, D] float32; the cache is updated in place."""
+        n_heads, G, D = q.shape
+        assert n_heads == cache.length.numel() and D == cache.K.shape[2] and q.dtype == cache.K.dtype and q.is_contiguous()
+        if k_new is not None:
+            assert k_new.shape == v_new.shape == (n_heads, D) and k_new.dtype == v_new.dtype == cache.K.dtype
+            assert pos.shape == (n_heads,) and pos.dtype == torch.int32
+        if out is None and want_out:
+            out = torch.empty(n_heads, G, D, dtype=torch.float32, device=q.device)
+        assert out is None or (out.shape == q.shape and out.dtype == torch.float32)
+        for t in (q, k_new, v_new, pos, out):
+            assert t is None or (t.is_contiguous() and t.device == cache.K.device)
+        self._check(self.lib.uncomp_paged_step(self.handle, self._paged(cache), q.data_ptr(), G, _ptr(k_new), _ptr(v_new), _ptr(pos),
+                                               _ptr(out), _stream(q.device)))
+        return out
+
+    def paged_evict(self, cache: PagedCache, budget: torch.Tensor, pos: torch.Tensor, w: int, evicted=None):
+        """budget / pos [n_heads] int32.  Heads above their budget give up the rows of lowest cum outside the w most recent positions;
+        returns evicted [n_heads] int32, the rows that left."""
+        if evicted is None:
+            evicted = torch.empty_like(cache.length)
+        for t in (budget, pos, evicted):
+            assert t.shape == cache.length.shape and t.dtype == torch.int32 and t.is_contiguous() and t.device == cache.K.device
+        self._check(self.lib.uncomp_paged_evict(self.handle, self._paged(cache), budget.data_ptr(), pos.data_ptr(), int(w),
+                                                evicted.data_ptr(), _stream(budget.device)))
+        return evicted

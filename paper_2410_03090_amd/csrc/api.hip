@@ -1,32 +1,14 @@
 // C interface of libuncomp: argument checks, workspace carving and kernel launches.
 // Every entry point validates on the host, launches on the caller's stream and returns a
 // status; nothing here synchronises or allocates after uncomp_create.
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <new>
 
-#include "common.h"
+#include "api_common.h"
 
 using namespace uncomp;
 
 namespace {
-
-uncomp_status fail(uncomp_ctx* ctx, uncomp_status st, const char* fmt, ...) {
-    if (ctx != nullptr) {
-        va_list ap;
-        va_start(ap, fmt);
-        vsnprintf(ctx->err, sizeof(ctx->err), fmt, ap);
-        va_end(ap);
-    }
-    return st;
-}
-
-uncomp_status hip_fail(uncomp_ctx* ctx, hipError_t e, const char* what) {
-    return fail(ctx, UNCOMP_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 constexpr size_t kDefaultWorkspace = 64ull << 20;
 // Where the regions of the prefill calls start.  Nothing lies before it (the decode step, which keeps nothing between calls, starts

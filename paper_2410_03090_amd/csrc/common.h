@@ -260,6 +260,62 @@ hipError_t launch_decode_step(const void* q, const void* k_new, const void* v_ne
                               void* Kc, void* Vc, int32_t* idx, float* cum, int32_t* len, float* out,
                               int32_t* evicted, const Env& env);
 
+// A paged cache as its kernels see it (DEVICE pointers; pages of 1 << shift rows).
+struct PagedCache {
+    void* K;
+    void* V;
+    int32_t* idx;
+    float* cum;
+    const int32_t* table;
+    int32_t* len;
+    int n_heads, n_pages, shift, max_pages;
+};
+struct PagedStepPlan {
+    int n_split;         // parts per head
+    int rows;            // rows a head's table has room for
+    size_t head_off;     // int2  [n_heads]: rows before and after
+    size_t ml_off;       // float [n_heads][n_split][G][2]
+    size_t acc_off;      // float [n_heads][n_split][G][D]
+    size_t logit_off;    // float [n_heads][rows][G]
+    size_t bytes;
+};
+PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows);
+struct PagedEvictPlan {
+    int pairs;           // most rows of one head that move
+    size_t count_off;    // int32 [n_heads]
+    size_t pair_off;     // int2  [n_heads][pairs]: to, from
+    size_t bytes;
+};
+PagedEvictPlan plan_paged_evict(int n_heads, int rows);
+size_t paged_append_bytes(int n_heads);
+hipError_t launch_paged_append(const PagedCache& c, const void* K, const void* V, const int32_t* idx, const float* cum, const int32_t* rows_in,
+                               int rows, int64_t head_bytes, int64_t row_bytes, int row_size, char* ws, const Env& env);
+hipError_t launch_paged_step(const PagedCache& c, const void* q, const void* k_new, const void* v_new, uncomp_dtype dt, const int32_t* pos, int G,
+                             int D, const PagedStepPlan& p, char* ws, float* out, const Env& env);
+hipError_t launch_paged_evict(const PagedCache& c, const int32_t* budget, const int32_t* pos, int w, int row_size, const PagedEvictPlan& p, char* ws,
+                              int32_t* evicted, const Env& env);
+
+// Packed or padded sequences of one attention call: rows of sequence s start at first[s] (0 without first) and number len[s],
+// or first[s + 1] - first[s], or all; elements of (sequence, head, row) at s * ss + h * sh + r * sr.
+struct AttnRows {
+    const int32_t* first;
+    const int32_t* len;
+    int rows;
+    int64_t ss, sh, sr;
+};
+struct PrefillArgs {
+    const void* Q;
+    const void* K;
+    const void* V;
+    void* out;
+    float* lse;          // may be NULL
+    int n_seq, H, G;
+    AttnRows q, k, v, o;
+    int64_t lse_ss, lse_sh;
+};
+size_t prefill_attention_bytes(int n_seq, int H, int G, int D, int q_rows, int k_rows);
+hipError_t launch_prefill_attention(const PrefillArgs& a, uncomp_dtype dt, int D, char* ws, size_t ws_bytes, const Env& env);
+
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // LDS a workgroup may use on gfx950 (160 KiB) and what a kernel gets without asking (64 KiB).

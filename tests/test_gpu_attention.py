@@ -1,0 +1,247 @@
+"""Prompt attention against the float64 oracle.
+
+Tolerances, per element, with size = sum_j p_j |v_j| and n keys:
+  logits   D products of exact bf16 (fp32: rounded) values summed in fp32: off by at most (D + 8) 2^-24 sum_d |q_d k_d| / sqrt(D) = e;
+  weights  e each way of the exponential and of the sum, n + 64 roundings of the running sums: (2 e + (n + 64) 2^-24) size;
+  bf16     the weights' rounding 2^-8 size, the result's 2^-8 |out| on top (fp32 outputs: neither);
+  lse      e, the sum's relative error (n + 64) 2^-24, and 2^-22 |lse| for the logarithm's scaling and its own rounding."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import uncomp_oracle as O
+from tests._util import to_f64
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2410_03090_amd import binding
+    c = binding.Context(0, 64 << 20)
+    yield c
+    c.close()
+
+
+def _check(q, k, v, out, lse, dtype, what):
+    """q [nq, D], k, v [nk, D], out [nq, D], lse [nq]: one query head of one sequence, host tensors."""
+    q, k, v, got, got_lse = (to_f64(t) for t in (q, k, v, out, lse))
+    D = q.shape[1]
+    ref, ref_lse, size = O.causal_attention(q, k, v)
+    if len(q) == 0:
+        return
+    n = len(k)
+    with np.errstate(invalid="ignore"):
+        e = (D + 8) * 2.0 ** -24 * (np.abs(q) @ np.abs(np.where(np.isfinite(k), k, 0.0)).T).max(axis=1, initial=0.0) / np.sqrt(D)
+        tol = (2 * e + (n + 64) * 2.0 ** -24)[:, None] * size
+        if dtype == torch.bfloat16:
+            tol = tol + 2.0 ** -8 * size
+            tol = tol + 2.0 ** -8 * (np.abs(ref) + tol)
+        lse_tol = e + (n + 64) * 2.0 ** -24 + 2.0 ** -22 * np.abs(ref_lse)
+        bad = ~((np.abs(got - ref) <= tol) | (got == ref) | (np.isnan(got) & np.isnan(ref)))
+        bad_lse = ~((np.abs(got_lse - ref_lse) <= lse_tol) | (got_lse == ref_lse) | (np.isnan(got_lse) & np.isnan(ref_lse)))
+    assert not bad.any(), f"{what}: row, feature {np.argwhere(bad)[0]}: {got[bad][0]} for {ref[bad][0]}, allowed {tol[bad][0]}"
+    assert not bad_lse.any(), f"{what}: lse of row {np.argwhere(bad_lse)[0]}: {got_lse[bad_lse][0]} for {ref_lse[bad_lse][0]}"
+
+
+def _packed(seqs, H, G, D, dtype, seed):
+    """Token-major projections [T, heads, D] seen head first, and the starts."""
+    g = torch.Generator().manual_seed(seed)
+    qs = np.cumsum([0] + [a for a, _ in seqs]).tolist()
+    ks = np.cumsum([0] + [b for _, b in seqs]).tolist()
+    Q = (1.3 * torch.randn(max(qs[-1], 1), H * G, D, generator=g)).to(dtype)
+    K, V = (torch.randn(max(ks[-1], 1), H, D, generator=g).to(dtype) for _ in range(2))
+    return Q.transpose(0, 1), K.transpose(0, 1), V.transpose(0, 1), qs, ks
+
+
+def _run_packed(ctx, Q, K, V, G, qs, ks):
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    out, lse = ctx.prefill_attention(Q.to(DEV), K.to(DEV), V.to(DEV), G, q_first=i32(qs), k_first=i32(ks))
+    torch.cuda.synchronize()
+    return out.cpu(), lse.cpu()
+
+
+def _check_packed(Q, K, V, G, qs, ks, out, lse, dtype, heads=None):
+    for s in range(len(qs) - 1):
+        for h in range(Q.shape[0]) if heads is None else heads:
+            a, b = slice(qs[s], qs[s + 1]), slice(ks[s], ks[s + 1])
+            _check(Q[h, a], K[h // G, b], V[h // G, b], out[h, a], lse[h, a], dtype, f"sequence {s}, head {h}")
+
+
+SEQS = [
+    [(1, 1)],
+    [(1, 300), (2, 2), (0, 5), (3, 1), (5, 0), (17, 17)],            # no queries, rows that see nothing, no keys
+    [(63, 63), (64, 64), (65, 65), (31, 95), (33, 33)],
+    [(130, 130), (7, 519), (1, 33), (200, 257)],
+    [(300, 300), (5, 3), (260, 1000), (513, 513)],
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,G,D", [(2, 1, 128), (1, 4, 128), (2, 7, 128), (2, 4, 64), (1, 8, 64), (3, 2, 128)])
+@pytest.mark.parametrize("seqs", range(len(SEQS)))
+def test_packed_sequences(ctx, dtype, H, G, D, seqs):
+    Q, K, V, qs, ks = _packed(SEQS[seqs], H, G, D, dtype, 10 * seqs + G)
+    out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
+    _check_packed(Q, K, V, G, qs, ks, out, lse, dtype)
+
+
+@pytest.mark.parametrize("dtype,G,D", [(torch.bfloat16, 4, 128), (torch.bfloat16, 3, 64), (torch.float32, 4, 128)])
+def test_padded_batch_with_lengths_and_strides(ctx, dtype, G, D):
+    """[B, H, N, D] with rows of its own spacing; rows behind a sequence's length hold NaN and its outputs there stay."""
+    B, H, Nq, Nk = 3, 2, 150, 190
+    q_len, k_len = [150, 1, 77], [190, 40, 77]
+    g = torch.Generator().manual_seed(3)
+    Q = torch.randn(B, H * G, Nq, D + 8, generator=g).to(dtype)[..., :D]
+    K = torch.randn(B, Nk, H, D, generator=g).to(dtype).transpose(1, 2)
+    V = torch.randn(H, B, Nk, D + 24, generator=g).to(dtype)[..., :D].transpose(0, 1)
+    for b in range(B):
+        Q[b, :, q_len[b]:] = float("nan")
+        K[b, :, k_len[b]:] = float("nan")
+        V[b, :, k_len[b]:] = float("nan")
+    dev = lambda t: torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=DEV).copy_(t)  # noqa: E731
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    out = torch.full((B, H * G, Nq, D), 7.0, dtype=dtype, device=DEV)
+    lse = torch.full((B, H * G, Nq), 7.0, device=DEV)
+    ctx.prefill_attention(dev(Q), dev(K), dev(V), G, q_len=i32(q_len), k_len=i32(k_len), out=out, lse=lse)
+    torch.cuda.synchronize()
+    out, lse = out.cpu(), lse.cpu()
+    for b in range(B):
+        assert (out[b, :, q_len[b]:] == 7.0).all() and (lse[b, :, q_len[b]:] == 7.0).all()
+        for h in range(H * G):
+            _check(Q[b, h, :q_len[b]], K[b, h // G, :k_len[b]], V[b, h // G, :k_len[b]], out[b, h, :q_len[b]], lse[b, h, :q_len[b]], dtype,
+                   f"batch {b}, head {h}")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_infinities_and_nan_touch_only_the_rows_that_see_them(ctx, dtype, D):
+    """A value of infinity, a NaN value, a NaN key, logits of -inf and +inf, in the middle of masked tiles and of whole ones."""
+    G, n = 2, 400
+    Q, K, V, qs, ks = _packed([(n, n)], 1, G, D, dtype, 5)
+    Q = Q.abs().contiguous()                                             # so that an infinite key feature is an infinite logit
+    V[0, 390, 3] = float("inf")
+    V[0, 391, 4] = float("-inf")
+    V[0, 350, 7] = float("nan")
+    K[0, 200, 1] = float("-inf")                                         # a key without weight
+    K[0, 380, 0] = float("nan")
+    out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
+    _check_packed(Q, K, V, G, qs, ks, out, lse, dtype)
+    K[0, :, 0] = float("-inf")                                           # no key has weight: as a row that sees nothing
+    K[0, 380, 0] = float("inf")
+    V = torch.randn(V.shape, generator=torch.Generator().manual_seed(6)).to(dtype)
+    out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
+    assert (out[:, :380] == 0).all() and (lse[:, :380] == float("-inf")).all()
+    assert out[:, 380:].isnan().all() and lse[:, 380:].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_large_logits(ctx, dtype):
+    """Logits of hundreds, growing along the keys: the running maximum moves in every block."""
+    G, n, D = 4, 600, 128
+    Q, K, V, qs, ks = _packed([(n, n)], 1, G, D, dtype, 8)
+    Q = (Q.abs() + 1.0).to(dtype)
+    K = (K.abs() * torch.linspace(0.01, 3.0, n)[None, :, None]).to(dtype)
+    out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
+    _check_packed(Q, K, V, G, qs, ks, out, lse, dtype)
+
+
+def test_long_context_of_few_queries(ctx):
+    G, D, dtype = 4, 128, torch.bfloat16
+    Q, K, V, qs, ks = _packed([(3, 20011), (40, 9000), (1, 1)], 1, G, D, dtype, 9)
+    out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
+    _check_packed(Q, K, V, G, qs, ks, out, lse, dtype)
+
+
+def test_shared_keys_starts_out_of_range_and_many_sequences(ctx):
+    """Two sequences over the same keys; lengths beyond the rows are cut; more sequences than lanes."""
+    G, D, H = 2, 64, 1
+    g = torch.Generator().manual_seed(11)
+    Q = torch.randn(H * G, 90, D, generator=g).to(torch.bfloat16)
+    K, V = (torch.randn(H, 100, D, generator=g).to(torch.bfloat16) for _ in range(2))
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    q_first, q_len = [0, 30, 80], [30, 50, 1000]
+    k_first, k_len = [10, 10, -5], [60, 60, 2000]
+    out, lse = ctx.prefill_attention(Q.to(DEV), K.to(DEV), V.to(DEV), G, q_first=i32(q_first), q_len=i32(q_len), k_first=i32(k_first),
+                                     k_len=i32(k_len))
+    torch.cuda.synchronize()
+    for qa, qb, ka, kb in ((0, 30, 10, 70), (30, 80, 10, 70), (80, 90, 0, 100)):
+        for h in range(G):
+            _check(Q[h, qa:qb], K[0, ka:kb], V[0, ka:kb], out[h, qa:qb].cpu(), lse[h, qa:qb].cpu(), torch.bfloat16, f"rows {qa}")
+    seqs = [((3 * s) % 7, (3 * s) % 7 + s % 3) for s in range(150)]
+    Q, K, V, qs, ks = _packed(seqs, H, G, D, torch.bfloat16, 12)
+    out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
+    _check_packed(Q, K, V, G, qs, ks, out, lse, torch.bfloat16)
+
+
+def test_graph_replays_on_new_contents_and_a_stream_of_its_own(ctx):
+    G, D, dtype = 4, 128, torch.bfloat16
+    Q, K, V, qs, ks = _packed([(100, 100), (9, 700)], 2, G, D, dtype, 13)
+    q, k, v = Q.to(DEV), K.to(DEV), V.to(DEV)
+    first = [torch.tensor(x, dtype=torch.int32, device=DEV) for x in (qs, ks)]
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:-1], device=DEV)
+    call = lambda: ctx.prefill_attention(q, k, v, G, q_first=first[0], k_first=first[1], out=out, lse=lse)  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for seed in (20, 21, 22):
+        Q, K, V, _, _ = _packed([(100, 100), (9, 700)], 2, G, D, dtype, seed)
+        q.copy_(Q), k.copy_(K), v.copy_(V)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone()
+        _check_packed(Q, K, V, G, qs, ks, out.cpu(), lse.cpu(), dtype, heads=[0, 7])
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+
+
+def test_normalisers_serve_the_window_score(ctx):
+    """A batch's attention leaves the lse that the score call takes over: the scores are those of the library's own pass."""
+    B, H, G, N, w, D = 2, 2, 4, 700, 32, 128
+    g = torch.Generator().manual_seed(14)
+    Q = torch.randn(B, H * G, N, D, generator=g).to(torch.bfloat16).to(DEV)
+    K, V = (torch.randn(B, H, N, D, generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    _, lse = ctx.prefill_attention(Q, K, V, G)
+    win = Q[:, :, N - w:].contiguous()
+    with_lse = ctx.window_score(win, K, G, lse=lse[:, :, N - w:].contiguous())
+    without = ctx.window_score(win, K, G)
+    torch.cuda.synchronize()
+    np.testing.assert_allclose(with_lse.cpu().numpy(), without.cpu().numpy(), rtol=4e-5)
+
+
+def test_refusals(ctx):
+    from paper_2410_03090_amd import binding
+    lib = binding.load_library()
+    c3, c2 = binding.ctypes.c_int64 * 3, binding.ctypes.c_int64 * 2
+    t = torch.zeros(1 << 16, dtype=torch.bfloat16, device=DEV)
+    out = torch.full((1 << 16,), 3.0, dtype=torch.bfloat16, device=DEV)
+
+    def call(**kw):
+        a = dict(ctx=ctx.handle, Q=t.data_ptr(), K=t.data_ptr(), V=t.data_ptr(), dtype=binding.BF16, n_seq=1, H=2, G=2, D=128, q_rows=16,
+                 k_rows=16, q_first=None, q_len=None, k_first=None, k_len=None, qs=c3(0, 128, 512), ks=c3(0, 128, 256), vs=c3(0, 128, 256),
+                 out=out.data_ptr(), os=c3(0, 128, 512), lse=None, ls=c2(0, 16), stream=None)
+        a.update(kw)
+        return lib.uncomp_prefill_attention(*a.values())
+
+    assert call(ctx=None) == binding.ERR_INVALID_ARG
+    for kw in (dict(Q=None), dict(K=None), dict(V=None), dict(out=None), dict(qs=None), dict(os=None), dict(n_seq=0), dict(H=-1), dict(G=0),
+               dict(q_rows=0), dict(k_rows=0), dict(qs=c3(0, 128, 120)), dict(ks=c3(0, 132, 256)), dict(vs=c3(-8, 128, 256)),
+               dict(os=c3(0, 128, 516)), dict(Q=t.data_ptr() + 2), dict(out=out.data_ptr() + 8), dict(lse=out.data_ptr(), ls=None),
+               dict(lse=out.data_ptr(), ls=c2(0, -1)), dict(lse=out.data_ptr() + 2), dict(q_len=t.data_ptr() + 1)):
+        assert call(**kw) == binding.ERR_INVALID_ARG, kw
+        assert b"prefill_attention" in lib.uncomp_last_error(ctx.handle)
+    for kw in (dict(dtype=2), dict(D=96), dict(D=256), dict(q_rows=1 << 30), dict(n_seq=(1 << 20) + 1), dict(H=1 << 21)):
+        assert call(**kw) == binding.ERR_UNSUPPORTED, kw
+    torch.cuda.synchronize()
+    assert (out == 3.0).all()
+    assert call() == binding.OK
+    torch.cuda.synchronize()
