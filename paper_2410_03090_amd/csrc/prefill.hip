@@ -234,10 +234,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
     const int col = c_wave + c, cc = min(col, last_col);
     const int qi = cc / G, head = h * G + cc % G;
     const int lim = off + qi;                                             // last key the lane's column sees
-    const int wave_all = off + min(c_wave, last_col) / G;                 // last key that all of the wave's columns see,
-    const int wave_end = min(nk, off + min(c_wave + 31, last_col) / G + 1);      // keys that any of them sees
     const int wg_all = off + c_wg / G, wg_end = min(nk, off + min(c_wg + kCols - 1, last_col) / G + 1);
     const int n_tiles = wg_end <= 0 ? 0 : (wg_end + kTileKeys - 1) / kTileKeys;
+    const int n_whole = wg_all < 0 ? 0 : min(nk, wg_all + 1) / kTileKeys;            // tiles that all columns see all of
     const float scale2 = kLog2eA * (D == 128 ? 0.08838834764831845f : 0.125f);
     const int q_first = __builtin_amdgcn_readfirstlane(w.q_first), k_first = __builtin_amdgcn_readfirstlane(w.k_first);
     const bf16_bits* Q = static_cast<const bf16_bits*>(a.Q) + s * a.q.ss + head * a.q.sh + (int64_t)(q_first + qi) * a.q.sr;
@@ -258,21 +257,24 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
         k_off[i] = row * (int)a.k.sr * 2 + piece * 16;
         v_off[i] = row * (int)a.v.sr * 2 + piece * 16;
     }
-    auto fetch = [&](int tile) {
-        const auto kr = rows_from(K, a.k.sr, tile * kTileKeys, nk, D), vr = rows_from(V, a.v.sr, tile * kTileKeys, nk, D);
+    auto fetch_keys = [&](int tile) {
+        const auto rows = rows_from(K, a.k.sr, tile * kTileKeys, nk, D);
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            kp[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kr, k_off[i], 0, 0));
-            vp[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(vr, v_off[i], 0, 0));
-        }
+        for (int i = 0; i < kMine; ++i) kp[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, k_off[i], 0, 0));
     };
-    auto stage = [&](int buf, int tile) {
+    auto fetch_values = [&](int tile) {
+        const auto rows = rows_from(V, a.v.sr, tile * kTileKeys, nk, D);
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            *reinterpret_cast<u32x4_t*>(&lds[buf][0][put[i]]) = kp[i];
-            *reinterpret_cast<u32x4_t*>(&lds[buf][1][put[i]]) = vp[i];
-        }
-        if (tile * kTileKeys + kTileKeys - 1 > wg_all) {                  // only tiles that some column does not see all of ask for it
+        for (int i = 0; i < kMine; ++i) vp[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, v_off[i], 0, 0));
+    };
+    auto stage_keys = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) *reinterpret_cast<u32x4_t*>(&lds[buf][0][put[i]]) = kp[i];
+    };
+    auto stage_values = [&](int buf, int tile) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) *reinterpret_cast<u32x4_t*>(&lds[buf][1][put[i]]) = vp[i];
+        if (tile >= n_whole) {                                            // only tiles that some column does not see all of ask for it
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < kMine; ++i)
@@ -282,43 +284,35 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
         }
     };
 
-    f32x16_t o[kBlocks];
+    f32x16_t o[kBlocks], z[2][2];                                         // output; logits of two tiles
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
+    for (int b = 0; b < kBlocks; ++b) o[b] = f32x16_t{};
     float m = -INFINITY, l = 0.f;                                         // maximum of the unscaled logits; this half's share of the sum
 
     const int k_row = c * kRowBytes, k_swap = piece_swap<D>(c);
     const int i16 = lane & 15, v_row = 4 * half + (i16 >> 2);
-    auto v_at = [&](int x, int b) {                                       // keys v_row + 8 x, features of block b
-        const int piece = 4 * b + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
-        return (v_row + 8 * x) * kRowBytes + (piece ^ piece_swap<D>(v_row + 8 * x)) * 16 + (i16 & 1) * 8;
+    auto key_operand = [&](int buf, int b, int i) {
+        const unsigned char* at = lds[buf][0] + 32 * b * kRowBytes + k_row + (((2 * i + half) ^ k_swap) << 4);
+        return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(at));
     };
-    auto compute = [&](int buf, int tile) {
-        const unsigned char* kt = lds[buf][0];
-        const unsigned char* vt = lds[buf][1];
-        const int k0 = tile * kTileKeys;
-        f32x16_t z[2];
+    auto value_operand = [&](int buf, int st, int b) {                    // keys 16 st ... of the tile, features of block b
+        s16x4_t v[2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) z[b][r] = 0.f;
+        for (int x = 0; x < 2; ++x) {
+            const int piece = 4 * b + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1), row = v_row + 8 * x;
+            v[x] = read_transposed(lds[buf][1] + (16 * st + row) * kRowBytes + (piece ^ piece_swap<D>(row)) * 16 + (i16 & 1) * 8);
+        }
+        return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto logits = [&](int buf, f32x16_t (&to)[2]) {
+        to[0] = f32x16_t{};
+        to[1] = f32x16_t{};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const u32x4_t k = *reinterpret_cast<const u32x4_t*>(kt + 32 * b * kRowBytes + k_row + (((2 * i + half) ^ k_swap) << 4));
-                z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), q[i], z[b], 0, 0, 0);
-            }
-        const bool masked = k0 + kTileKeys - 1 > wave_all;
-        if (masked) {
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (k0 + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3) > lim) z[b][r] = -INFINITY;
-        }
+            for (int b = 0; b < 2; ++b) to[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(buf, b, i), q[i], to[b], 0, 0, 0);
+    };
+    auto follow = [&](const f32x16_t (&z)[2]) {
         float top = z[0][0];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -338,16 +332,41 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
                 for (int r = 0; r < 16; ++r) o[b][r] *= f;
             m = m_new;
         }
+    };
+    auto weights = [&](const f32x16_t (&z)[2], bf16x8_t (&p)[4]) {
         const float ref = reference(m) * scale2;
-        bf16x8_t p[4];
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const float e = __builtin_amdgcn_exp2f(fmaf(z[b][r], scale2, -ref));
-                l += e;
+                sum[r & 3] += e;
                 p[2 * b + (r >> 3)][r & 7] = (__bf16)e;
             }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+    // One tile: its logits are there.  The next tile's are made beside its weights: products for the matrix cores, exponentials for the
+    // vector unit, neither waiting for the other.
+    auto turn = [&](auto BUF, auto MASKED, int tile) {
+        constexpr int buf = decltype(BUF)::value;
+        constexpr bool masked = decltype(MASKED)::value;
+        stage_keys(buf);                                                  // tile + 2
+        fetch_keys(tile + 3);
+        stage_values(buf ^ 1, tile + 1);
+        fetch_values(tile + 2);
+        if constexpr (masked) {
+            const int k0 = tile * kTileKeys;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (k0 + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3) > lim) z[buf][b][r] = -INFINITY;
+        }
+        follow(z[buf]);
+        bf16x8_t p[4];
+        weights(z[buf], p);
+        logits(buf ^ 1, z[buf ^ 1]);
         if (masked && not_finite[buf] == tile + 1) {
             // Zero times infinity or NaN is NaN: the keys are taken one at a time, and columns that do not see one keep what they had.
 #pragma unroll
@@ -355,7 +374,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
 #pragma unroll 1
                 for (int k = 0; k < 16; ++k) {                            // key 16 st + k: half k / 4 % 2, slot k % 4 + 4 (k / 8)
                     const int slot = (k & 3) + 4 * (k >> 3);
-                    const bool here = half == ((k >> 2) & 1), seen = k0 + 16 * st + k <= lim;
+                    const bool here = half == ((k >> 2) & 1), seen = tile * kTileKeys + 16 * st + k <= lim;
                     u32x4_t one = __builtin_bit_cast(u32x4_t, p[st]), keep;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -364,8 +383,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
                     }
 #pragma unroll
                     for (int b = 0; b < kBlocks; ++b) {
-                        const s16x4_t lo = read_transposed(vt + v_at(0, b) + 16 * st * kRowBytes), hi = read_transposed(vt + v_at(1, b) + 16 * st * kRowBytes);
-                        u32x4_t v = __builtin_bit_cast(u32x4_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                        u32x4_t v = __builtin_bit_cast(u32x4_t, value_operand(buf, st, b));
 #pragma unroll
                         for (int e = 0; e < 4; ++e) v[e] &= keep[e];
                         const f32x16_t next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, one),
@@ -378,32 +396,35 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
 #pragma unroll
             for (int st = 0; st < 4; ++st)
 #pragma unroll
-                for (int b = 0; b < kBlocks; ++b) {
-                    const s16x4_t lo = read_transposed(vt + v_at(0, b) + 16 * st * kRowBytes), hi = read_transposed(vt + v_at(1, b) + 16 * st * kRowBytes);
-                    const auto v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), p[st], o[b], 0, 0, 0);
-                }
+                for (int b = 0; b < kBlocks; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_operand(buf, st, b), p[st], o[b], 0, 0, 0);
         }
+        __syncthreads();
     };
 
     if (n_tiles > 0) {
+        using I0 = std::integral_constant<int, 0>;
+        using I1 = std::integral_constant<int, 1>;
         if (tid < 2) not_finite[tid] = 0;
         __syncthreads();
-        fetch(0);
-        stage(0, 0);
-        fetch(1);
+        fetch_keys(0);
+        fetch_values(0);
+        stage_keys(0);
+        stage_values(0, 0);
+        fetch_keys(1);
+        fetch_values(1);
+        stage_keys(1);
+        fetch_keys(2);
         __syncthreads();
-        auto turn = [&](int buf, int tile) {
-            if (tile + 1 < n_tiles) {
-                stage(buf ^ 1, tile + 1);
-                fetch(tile + 2);
-            }
-            if (tile * kTileKeys < wave_end) compute(buf, tile);
-            __syncthreads();
-        };
-        for (int tile = 0; tile < n_tiles; tile += 2) {
-            turn(0, tile);
-            if (tile + 1 < n_tiles) turn(1, tile + 1);
+        logits(0, z[0]);
+        __syncthreads();
+        int tile = 0;
+        for (; tile + 1 < n_whole; tile += 2) {
+            turn(I0{}, std::false_type{}, tile);
+            turn(I1{}, std::false_type{}, tile + 1);
+        }
+        for (; tile < n_tiles; tile += 2) {
+            turn(I0{}, std::true_type{}, tile);
+            if (tile + 1 < n_tiles) turn(I1{}, std::true_type{}, tile + 1);
         }
     }
     const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
