@@ -234,6 +234,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
     const int col = c_wave + c, cc = min(col, last_col);
     const int qi = cc / G, head = h * G + cc % G;
     const int lim = off + qi;                                             // last key the lane's column sees
+    const int wave_end = min(nk, off + min(c_wave + 31, last_col) / G + 1);      // keys that any of the wave's columns sees
     const int wg_all = off + c_wg / G, wg_end = min(nk, off + min(c_wg + kCols - 1, last_col) / G + 1);
     const int n_tiles = wg_end <= 0 ? 0 : (wg_end + kTileKeys - 1) / kTileKeys;
     const int n_whole = wg_all < 0 ? 0 : min(nk, wg_all + 1) / kTileKeys;            // tiles that all columns see all of
@@ -257,21 +258,21 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
         k_off[i] = row * (int)a.k.sr * 2 + piece * 16;
         v_off[i] = row * (int)a.v.sr * 2 + piece * 16;
     }
-    auto fetch_keys = [&](int tile) {
+    auto fetch_keys = [&](int tile) __attribute__((always_inline)) {
         const auto rows = rows_from(K, a.k.sr, tile * kTileKeys, nk, D);
 #pragma unroll
         for (int i = 0; i < kMine; ++i) kp[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, k_off[i], 0, 0));
     };
-    auto fetch_values = [&](int tile) {
+    auto fetch_values = [&](int tile) __attribute__((always_inline)) {
         const auto rows = rows_from(V, a.v.sr, tile * kTileKeys, nk, D);
 #pragma unroll
         for (int i = 0; i < kMine; ++i) vp[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, v_off[i], 0, 0));
     };
-    auto stage_keys = [&](int buf) {
+    auto stage_keys = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kMine; ++i) *reinterpret_cast<u32x4_t*>(&lds[buf][0][put[i]]) = kp[i];
     };
-    auto stage_values = [&](int buf, int tile) {
+    auto stage_values = [&](int buf, int tile) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kMine; ++i) *reinterpret_cast<u32x4_t*>(&lds[buf][1][put[i]]) = vp[i];
         if (tile >= n_whole) {                                            // only tiles that some column does not see all of ask for it
@@ -284,18 +285,18 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
         }
     };
 
-    f32x16_t o[kBlocks], z[2][2];                                         // output; logits of two tiles
+    f32x16_t o[kBlocks], z[2];                                            // output; logits of two blocks of 32 keys
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) o[b] = f32x16_t{};
     float m = -INFINITY, l = 0.f;                                         // maximum of the unscaled logits; this half's share of the sum
 
     const int k_row = c * kRowBytes, k_swap = piece_swap<D>(c);
     const int i16 = lane & 15, v_row = 4 * half + (i16 >> 2);
-    auto key_operand = [&](int buf, int b, int i) {
+    auto key_operand = [&](int buf, int b, int i) __attribute__((always_inline)) {
         const unsigned char* at = lds[buf][0] + 32 * b * kRowBytes + k_row + (((2 * i + half) ^ k_swap) << 4);
         return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(at));
     };
-    auto value_operand = [&](int buf, int st, int b) {                    // keys 16 st ... of the tile, features of block b
+    auto value_operand = [&](int buf, int st, int b) __attribute__((always_inline)) {                    // keys 16 st ... of the tile, features of block b
         s16x4_t v[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -304,20 +305,15 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
         }
         return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    auto logits = [&](int buf, f32x16_t (&to)[2]) {
-        to[0] = f32x16_t{};
-        to[1] = f32x16_t{};
+    auto logits = [&](int buf, int b, f32x16_t& to) __attribute__((always_inline)) {
+        to = f32x16_t{};
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) to[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(buf, b, i), q[i], to[b], 0, 0, 0);
+        for (int i = 0; i < kSteps; ++i) to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_operand(buf, b, i), q[i], to, 0, 0, 0);
     };
-    auto follow = [&](const f32x16_t (&z)[2]) {
-        float top = z[0][0];
+    auto follow = [&](const f32x16_t& z) __attribute__((always_inline)) {
+        float top = z[0];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, z[b][r]);
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, z[r]);
         const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1]));
         // The reference follows the maximum when that has grown by more than a factor of 2^8 of the weights: until then they are
@@ -333,72 +329,84 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
             m = m_new;
         }
     };
-    auto weights = [&](const f32x16_t (&z)[2], bf16x8_t (&p)[4]) {
+    auto weights = [&](const f32x16_t& z, bf16x8_t (&p)[2]) __attribute__((always_inline)) {
         const float ref = reference(m) * scale2;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(z[b][r], scale2, -ref));
-                sum[r & 3] += e;
-                p[2 * b + (r >> 3)][r & 7] = (__bf16)e;
-            }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        for (int r = 0; r < 16; ++r) {
+            const float e = __builtin_amdgcn_exp2f(fmaf(z[r], scale2, -ref));
+            sum[r & 1] += e;
+            p[r >> 3][r & 7] = (__bf16)e;
+        }
+        l += sum[0] + sum[1];
     };
-    // One tile: its logits are there.  The next tile's are made beside its weights: products for the matrix cores, exponentials for the
-    // vector unit, neither waiting for the other.
-    auto turn = [&](auto BUF, auto MASKED, int tile) {
+    // what the column does not see among 32 keys from k0 on
+    auto mask = [&](f32x16_t& z, int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (k0 + 8 * (r >> 2) + 4 * half + (r & 3) > lim) z[r] = -INFINITY;
+    };
+    auto add_values = [&](int buf, int blk, const bf16x8_t (&p)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_operand(buf, 2 * blk + st, b), p[st], o[b], 0, 0, 0);
+    };
+    // Zero times infinity or NaN is NaN: the keys are taken one at a time, and columns that do not see one keep what they had.
+    auto add_values_one_by_one = [&](int buf, int blk, const bf16x8_t (&p)[2], int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll 1
+            for (int k = 0; k < 16; ++k) {                                // key 16 st + k: half k / 4 % 2, slot k % 4 + 4 (k / 8)
+                const int slot = (k & 3) + 4 * (k >> 3);
+                const bool here = half == ((k >> 2) & 1), seen = k0 + 16 * st + k <= lim;
+                u32x4_t one = __builtin_bit_cast(u32x4_t, p[st]), keep;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    keep[e] = here && (slot >> 1) == e ? ((slot & 1) ? 0xffff0000u : 0xffffu) : 0u;
+                    one[e] &= keep[e];
+                }
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    u32x4_t v = __builtin_bit_cast(u32x4_t, value_operand(buf, 2 * blk + st, b));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] &= keep[e];
+                    const f32x16_t next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, one),
+                                                                                   o[b], 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[b][r] = seen ? next[r] : o[b][r];
+                }
+            }
+    };
+    // One turn of the loop, in units of 32 keys: the outputs of a tile's two units, the weights of its second and of the next tile's
+    // first, the logits of the next tile's two.  A unit's logits are made beside the weights of the one before and its maximum
+    // beside the outputs of that one, so that the matrix cores and the vector unit have independent work.  All reads of a
+    // tile's keys, and of its values, lie between two barriers: keys one tile ahead of the values.
+    bf16x8_t p[2];
+    auto turn = [&](auto BUF, auto MASKED, int tile) __attribute__((always_inline)) {
         constexpr int buf = decltype(BUF)::value;
         constexpr bool masked = decltype(MASKED)::value;
+        __syncthreads();
         stage_keys(buf);                                                  // tile + 2
         fetch_keys(tile + 3);
         stage_values(buf ^ 1, tile + 1);
         fetch_values(tile + 2);
-        if constexpr (masked) {
-            const int k0 = tile * kTileKeys;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (k0 + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3) > lim) z[buf][b][r] = -INFINITY;
-        }
-        follow(z[buf]);
-        bf16x8_t p[4];
-        weights(z[buf], p);
-        logits(buf ^ 1, z[buf ^ 1]);
-        if (masked && not_finite[buf] == tile + 1) {
-            // Zero times infinity or NaN is NaN: the keys are taken one at a time, and columns that do not see one keep what they had.
-#pragma unroll
-            for (int st = 0; st < 4; ++st)
-#pragma unroll 1
-                for (int k = 0; k < 16; ++k) {                            // key 16 st + k: half k / 4 % 2, slot k % 4 + 4 (k / 8)
-                    const int slot = (k & 3) + 4 * (k >> 3);
-                    const bool here = half == ((k >> 2) & 1), seen = tile * kTileKeys + 16 * st + k <= lim;
-                    u32x4_t one = __builtin_bit_cast(u32x4_t, p[st]), keep;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        keep[e] = here && (slot >> 1) == e ? ((slot & 1) ? 0xffff0000u : 0xffffu) : 0u;
-                        one[e] &= keep[e];
-                    }
-#pragma unroll
-                    for (int b = 0; b < kBlocks; ++b) {
-                        u32x4_t v = __builtin_bit_cast(u32x4_t, value_operand(buf, st, b));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] &= keep[e];
-                        const f32x16_t next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, one),
-                                                                                       o[b], 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) o[b][r] = seen ? next[r] : o[b][r];
-                    }
-                }
-        } else {
-#pragma unroll
-            for (int st = 0; st < 4; ++st)
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_operand(buf, st, b), p[st], o[b], 0, 0, 0);
-        }
-        __syncthreads();
+        const int k0 = tile * kTileKeys;
+        if (masked && k0 >= wave_end) return;
+        const bool odd_values = masked && not_finite[buf] == tile + 1;
+        if (odd_values) add_values_one_by_one(buf, 0, p, k0);
+        else add_values(buf, 0, p);
+        if constexpr (masked) mask(z[1], k0 + 32);
+        follow(z[1]);
+        logits(buf ^ 1, 0, z[0]);
+        weights(z[1], p);
+        if (odd_values) add_values_one_by_one(buf, 1, p, k0 + 32);
+        else add_values(buf, 1, p);
+        if constexpr (masked) mask(z[0], k0 + 64);
+        follow(z[0]);
+        logits(buf ^ 1, 1, z[1]);
+        weights(z[0], p);
     };
 
     if (n_tiles > 0) {
@@ -415,10 +423,13 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
         stage_keys(1);
         fetch_keys(2);
         __syncthreads();
-        logits(0, z[0]);
-        __syncthreads();
+        logits(0, 0, z[0]);
+        mask(z[0], 0);
+        follow(z[0]);
+        logits(0, 1, z[1]);
+        weights(z[0], p);
         int tile = 0;
-        for (; tile + 1 < n_whole; tile += 2) {
+        for (; tile + 2 < n_whole; tile += 2) {
             turn(I0{}, std::false_type{}, tile);
             turn(I1{}, std::false_type{}, tile + 1);
         }
