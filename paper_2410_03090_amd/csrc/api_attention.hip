@@ -96,6 +96,7 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
         return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
     if (!strides_ok(q_strides, D) || !strides_ok(k_strides, D) || !strides_ok(v_strides, D) || !strides_ok(out_strides, D))
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: strides must be multiples of 8 elements, none negative, row strides >= D", who);
+    if (k_strides[2] >= 1 << 24 || v_strides[2] >= 1 << 24) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: row strides below 2^24 elements", who);
     if (lse_out != nullptr && (lse_strides[0] < 0 || lse_strides[1] < 0))
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: negative lse stride", who);
     if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(out) || !aligned4(lse_out) || !aligned4(q_first) || !aligned4(q_len) ||
@@ -118,8 +119,9 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
         a.lse_ss = lse_strides[0];
         a.lse_sh = lse_strides[1];
     }
-    const size_t need = prefill_attention_bytes(n_seq, H, G, D, q_rows, k_rows);
-    uncomp_status st = take_workspace(ctx, who, need, stream);
+    if (!prefill_attention_fits(a, dtype, D)) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
+    // what the call leaves in the workspace is as much as fits there
+    uncomp_status st = take_workspace(ctx, who, ctx->ws_bytes, stream);
     if (st != UNCOMP_OK) return st;
     OnDevice on(ctx->device);
     if (on.err != hipSuccess) return hip_fail(ctx, on.err, who);

@@ -9,10 +9,9 @@
 //   output    O^T = V^T P^T: the lane loads features c D / 16 ... of its own eight (four) value rows and pairs the bf16 of two
 //             rows up by byte permutes; the t-th product yields the features D / 16 * i + t, i = 0 ... 15.
 //
-// bf16 weights of outputs in 32 bits (FULL) are the sum of three bf16: twice the upper half of what is left of a float, shrunk a
-// little first so that no term is zero (zero times an infinite value is NaN, the weight times it is infinite), then the rest,
-// which rounding leaves within 2^-21 of the weight.  One term otherwise, which is off by at most the half step of bf16 that
-// the output is rounded by anyway.  Logits, maxima, sums and outputs are fp32.
+// Outputs are fp32, so bf16 weights are the sum of three bf16: twice the upper half of what is left of a float, shrunk a little
+// first so that no term is zero (zero times an infinite value is NaN, the weight times it is infinite), then the rest, which
+// rounding leaves within 2^-21 of the weight.  Logits, maxima and sums are fp32.
 #pragma once
 
 #include "device_utils.h"
@@ -57,17 +56,15 @@ __device__ __forceinline__ Words<N> load_words(const void* p) {
     return r;
 }
 
-template <typename T, int D, bool FULL>
+template <typename T, int D>
 struct WaveAttend;
 
 // ---- bf16: blocks of 32 keys ---------------------------------------------------------------------------------------
-template <int D, bool FULL>
-struct WaveAttend<bf16_bits, D, FULL> {
+template <int D>
+struct WaveAttend<bf16_bits, D> {
     static constexpr int kBlock = 32, kPerLane = 8, kSteps = D / 32, kVw = D / 16;
-    struct Rows {
-        Words<4> k[2][kSteps];
-        Words<kVw / 2> v[8];
-    };
+    struct Keys { Words<4> w[2][kSteps]; };
+    struct Values { Words<kVw / 2> w[8]; };
     bf16x8_t q[kSteps];
     f32x4_t o[kVw];
     float m, l;                        // running maximum (base 2), this lane's share of the running sum
@@ -88,89 +85,69 @@ struct WaveAttend<bf16_bits, D, FULL> {
     }
     static __device__ __forceinline__ int key_row(int lane, int tile) { return 8 * ((lane & 15) >> 2) + 4 * tile + (lane & 3); }
     static __device__ __forceinline__ int value_row(int lane, int e) { return 8 * (lane >> 4) + e; }
-    // krow / vrow (row of the block) -> the row's address
-    template <typename FK, typename FV>
-    static __device__ __forceinline__ void load(Rows& r, int lane, FK&& krow, FV&& vrow) {
+    // row (of the block) -> the row's address
+    template <typename F>
+    static __device__ __forceinline__ void load_keys(Keys& k, int lane, F&& row) {
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-            const bf16_bits* p = krow(key_row(lane, a));
+            const bf16_bits* p = row(key_row(lane, a));
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) r.k[a][s] = load_words<4>(p + 32 * s + 8 * (lane >> 4));
+            for (int s = 0; s < kSteps; ++s) k.w[a][s] = load_words<4>(p + 32 * s + 8 * (lane >> 4));
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r.v[e] = load_words<kVw / 2>(vrow(value_row(lane, e)) + kVw * (lane & 15));
     }
-    // value rows from n on are zeros (what lies there is nobody's)
-    static __device__ __forceinline__ void clear_values(Rows& r, int lane, int n) {
+    template <typename F>
+    static __device__ __forceinline__ void load_values(Values& v, int lane, F&& row) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (value_row(lane, e) >= n)
-#pragma unroll
-                for (int i = 0; i < kVw / 2; ++i) r.v[e].w[i] = 0u;
+        for (int e = 0; e < 8; ++e) v.w[e] = load_words<kVw / 2>(row(value_row(lane, e)) + kVw * (lane & 15));
     }
-    static __device__ __forceinline__ void clear_value(Rows& r, int e) {
+    static __device__ __forceinline__ void clear_value(Values& v, int e) {
 #pragma unroll
-        for (int i = 0; i < kVw / 2; ++i) r.v[e].w[i] = 0u;
+        for (int i = 0; i < kVw / 2; ++i) v.w[e].w[i] = 0u;
     }
-    __device__ __forceinline__ void logits(const Rows& r, float scale2, float (&s)[kPerLane]) const {
+    __device__ __forceinline__ void logits(const Keys& k, float scale2, float (&s)[kPerLane]) const {
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
             f32x4_t c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int t = 0; t < kSteps; ++t)
-                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, r.k[a][t]), q[t], c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k.w[a][t]), q[t], c, 0, 0, 0);
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[4 * a + e] = c[e] * scale2;
         }
     }
     // the t-th product's value operand
-    static __device__ __forceinline__ bf16x8_t value_operand(const Rows& r, int t) {
+    static __device__ __forceinline__ bf16x8_t value_operand(const Values& v, int t) {
         Words<4> a;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            a.w[e] = __builtin_amdgcn_perm(r.v[2 * e + 1].w[t >> 1], r.v[2 * e].w[t >> 1], (t & 1) ? 0x07060302u : 0x05040100u);
+            a.w[e] = __builtin_amdgcn_perm(v.w[2 * e + 1].w[t >> 1], v.w[2 * e].w[t >> 1], (t & 1) ? 0x07060302u : 0x05040100u);
         return __builtin_bit_cast(bf16x8_t, a);
     }
-    __device__ __forceinline__ void add_values(const Rows& r, const float (&p)[kPerLane]) {
+    __device__ __forceinline__ void add_values(const Values& v, const float (&p)[kPerLane]) {
         constexpr float kShrink = 1.f - 0x1p-8f;
-        bf16x8_t w[FULL ? 3 : 1];
+        bf16x8_t w[3];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if constexpr (FULL) {
-                const float a = upper_half(p[e] * kShrink), b = upper_half((p[e] - a) * kShrink);
-                w[0][e] = (__bf16)a;
-                w[1][e] = (__bf16)b;
-                w[2][e] = (__bf16)((p[e] - a) - b);
-            } else {
-                w[0][e] = (__bf16)p[e];
-            }
+            const float a = upper_half(p[e] * kShrink), b = upper_half((p[e] - a) * kShrink);
+            w[0][e] = (__bf16)a;
+            w[1][e] = (__bf16)b;
+            w[2][e] = (__bf16)((p[e] - a) - b);
         }
 #pragma unroll
         for (int t = 0; t < kVw; ++t) {
-            const bf16x8_t a = value_operand(r, t);
+            const bf16x8_t a = value_operand(v, t);
 #pragma unroll
-            for (int i = 0; i < (FULL ? 3 : 1); ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[i], o[t], 0, 0, 0);
+            for (int i = 0; i < 3; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[i], o[t], 0, 0, 0);
         }
-    }
-    static __device__ __forceinline__ bool values_finite(const Rows& r) {
-        bool bad = false;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int i = 0; i < kVw / 2; ++i)
-                bad |= (r.v[e].w[i] & 0x7f80u) == 0x7f80u || (r.v[e].w[i] & 0x7f800000u) == 0x7f800000u;
-        return !bad;
     }
 };
 
 // ---- fp32: blocks of 16 keys ---------------------------------------------------------------------------------------
-template <int D, bool FULL>
-struct WaveAttend<float, D, FULL> {
+template <int D>
+struct WaveAttend<float, D> {
     static constexpr int kBlock = 16, kPerLane = 4, kSteps = D / 16, kVw = D / 16;
-    struct Rows {
-        f32x4_t k[kSteps];
-        f32x4_t v[4][kVw / 4];
-    };
+    struct Keys { f32x4_t w[kSteps]; };
+    struct Values { f32x4_t w[4][kVw / 4]; };
     f32x4_t q[kSteps];
     f32x4_t o[kVw];
     float m, l;
@@ -188,50 +165,54 @@ struct WaveAttend<float, D, FULL> {
     }
     static __device__ __forceinline__ int key_row(int lane, int) { return lane & 15; }
     static __device__ __forceinline__ int value_row(int lane, int e) { return 4 * (lane >> 4) + e; }
-    template <typename FK, typename FV>
-    static __device__ __forceinline__ void load(Rows& r, int lane, FK&& krow, FV&& vrow) {
-        const float* p = krow(key_row(lane, 0));
+    template <typename F>
+    static __device__ __forceinline__ void load_keys(Keys& k, int lane, F&& row) {
+        const float* p = row(key_row(lane, 0));
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) r.k[s] = *reinterpret_cast<const f32x4_t*>(p + 16 * s + 4 * (lane >> 4));
+        for (int s = 0; s < kSteps; ++s) k.w[s] = *reinterpret_cast<const f32x4_t*>(p + 16 * s + 4 * (lane >> 4));
+    }
+    template <typename F>
+    static __device__ __forceinline__ void load_values(Values& v, int lane, F&& row) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float* v = vrow(value_row(lane, e)) + kVw * (lane & 15);
+            const float* p = row(value_row(lane, e)) + kVw * (lane & 15);
 #pragma unroll
-            for (int i = 0; i < kVw / 4; ++i) r.v[e][i] = *reinterpret_cast<const f32x4_t*>(v + 4 * i);
+            for (int i = 0; i < kVw / 4; ++i) v.w[e][i] = *reinterpret_cast<const f32x4_t*>(p + 4 * i);
         }
     }
-    static __device__ __forceinline__ void clear_values(Rows& r, int lane, int n) {
+    // value rows from n on are zeros (what lies there is nobody's)
+    static __device__ __forceinline__ void clear_values(Values& v, int lane, int n) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (value_row(lane, e) >= n)
 #pragma unroll
-                for (int i = 0; i < kVw / 4; ++i) r.v[e][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < kVw / 4; ++i) v.w[e][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    static __device__ __forceinline__ void clear_value(Rows& r, int e) {
+    static __device__ __forceinline__ void clear_value(Values& v, int e) {
 #pragma unroll
-        for (int i = 0; i < kVw / 4; ++i) r.v[e][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < kVw / 4; ++i) v.w[e][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    __device__ __forceinline__ void logits(const Rows& r, float scale2, float (&s)[kPerLane]) const {
+    __device__ __forceinline__ void logits(const Keys& k, float scale2, float (&s)[kPerLane]) const {
         f32x4_t c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < kSteps; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(r.k[t][e], q[t][e], c, 0, 0, 0);
+            for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(k.w[t][e], q[t][e], c, 0, 0, 0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] = c[e] * scale2;
     }
-    __device__ __forceinline__ void add_values(const Rows& r, const float (&p)[kPerLane]) {
+    __device__ __forceinline__ void add_values(const Values& v, const float (&p)[kPerLane]) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int t = 0; t < kVw; ++t) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(r.v[e][t >> 2][t & 3], p[e], o[t], 0, 0, 0);
+            for (int t = 0; t < kVw; ++t) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.w[e][t >> 2][t & 3], p[e], o[t], 0, 0, 0);
     }
-    static __device__ __forceinline__ bool values_finite(const Rows& r) {
+    static __device__ __forceinline__ bool values_finite(const Values& v) {
         bool bad = false;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int i = 0; i < kVw; ++i) bad |= (__float_as_uint(r.v[e][i >> 2][i & 3]) & 0x7f800000u) == 0x7f800000u;
+            for (int i = 0; i < kVw; ++i) bad |= (__float_as_uint(v.w[e][i >> 2][i & 3]) & 0x7f800000u) == 0x7f800000u;
         return !bad;
     }
 };
@@ -264,15 +245,15 @@ __device__ __forceinline__ void take_logits(A& a, float (&s)[A::kPerLane]) {
 // times infinity or NaN is NaN: with such values about, the rows are taken one at a time and the columns that do not see one keep
 // what they had.  sees(row of the block): whether the lane's column does.
 template <typename A, typename F>
-__device__ __forceinline__ void add_masked_values(A& a, const typename A::Rows& r, const float (&p)[A::kPerLane], int lane, F&& sees) {
-    if (!__any(!A::values_finite(r))) {
-        a.add_values(r, p);
+__device__ __forceinline__ void add_masked_values(A& a, const typename A::Values& v, const float (&p)[A::kPerLane], int lane, F&& sees) {
+    if (!__any(!A::values_finite(v))) {
+        a.add_values(v, p);
         return;
     }
 #pragma unroll 1
     for (int row = 0; row < 4 * A::kPerLane; ++row) {
         const int e = row % A::kPerLane;
-        typename A::Rows one = r;
+        typename A::Values one = v;
         float pe[A::kPerLane];
 #pragma unroll
         for (int f = 0; f < A::kPerLane; ++f) {

@@ -312,7 +312,12 @@ struct PrefillArgs {
     int n_seq, H, G;
     AttnRows q, k, v, o;
     int64_t lse_ss, lse_sh;
+    int n_split, target, least;      // parts that a tile's keys may be cut into; workgroups to have; blocks of 64 keys in a part
+    unsigned items;      // tiles of all KV heads, at most
+    float2* part_ml;     // where parts leave (maximum, sum) and outputs
+    float* part_acc;
 };
+bool prefill_attention_fits(const PrefillArgs& a, uncomp_dtype dt, int D);       // the launch's grid
 size_t prefill_attention_bytes(int n_seq, int H, int G, int D, int q_rows, int k_rows);
 hipError_t launch_prefill_attention(const PrefillArgs& a, uncomp_dtype dt, int D, char* ws, size_t ws_bytes, const Env& env);
 

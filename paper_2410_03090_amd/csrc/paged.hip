@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void paged_copy_kernel(PagedCache c, const cha
 template <typename T, int D>
 __global__ __launch_bounds__(kAttendThreads) void paged_attend_kernel(PagedCache c, const T* __restrict__ q, const T* __restrict__ k_new,
                                                                       const T* __restrict__ v_new, int G, int n_split, PagedStepPlan p, char* ws) {
-    using A = WaveAttend<T, D, true>;
+    using A = WaveAttend<T, D>;
     constexpr int kVw = A::kVw;
     __shared__ float o_s[kAttendWaves][16][D];
     __shared__ float ml_s[kAttendWaves][16][2];
@@ -125,21 +125,23 @@ __global__ __launch_bounds__(kAttendThreads) void paged_attend_kernel(PagedCache
             const int id = r < 16 ? id0 : id1;
             return ((int64_t)id << c.shift) + ((r0 + r) & in_page);
         };
-        typename A::Rows rows;
+        typename A::Keys keys;
+        typename A::Values values;
         float s[A::kPerLane];
         const bool whole = r0 + A::kBlock <= n && ok0 && ok1;
         if (whole) {
-            A::load(rows, lane, [&](int r) { return K + row_of(r) * D; }, [&](int r) { return V + row_of(r) * D; });
-            a.logits(rows, scale2, s);
+            A::load_keys(keys, lane, [&](int r) { return K + row_of(r) * D; });
+            A::load_values(values, lane, [&](int r) { return V + row_of(r) * D; });
+            a.logits(keys, scale2, s);
         } else {
             // rows behind the last, rows without a page (the pool's first row is read in their place) and the new token
             auto there = [&](int r) { return r0 + r < n ? (r < 16 ? ok0 : ok1) : joins && r0 + r == n; };
-            A::load(rows, lane, [&](int r) { return !there(r) ? K : r0 + r == n ? kn : K + row_of(r) * D; },
-                    [&](int r) { return !there(r) ? V : r0 + r == n ? vn : V + row_of(r) * D; });
+            A::load_keys(keys, lane, [&](int r) { return !there(r) ? K : r0 + r == n ? kn : K + row_of(r) * D; });
+            A::load_values(values, lane, [&](int r) { return !there(r) ? V : r0 + r == n ? vn : V + row_of(r) * D; });
 #pragma unroll
             for (int e = 0; e < A::kPerLane; ++e)
-                if (!there(A::value_row(lane, e))) A::clear_value(rows, e);
-            a.logits(rows, scale2, s);
+                if (!there(A::value_row(lane, e))) A::clear_value(values, e);
+            a.logits(keys, scale2, s);
 #pragma unroll
             for (int e = 0; e < A::kPerLane; ++e)
                 if (!there(A::value_row(lane, e))) s[e] = -INFINITY;
@@ -152,7 +154,7 @@ __global__ __launch_bounds__(kAttendThreads) void paged_attend_kernel(PagedCache
             }
         }
         take_logits(a, s);
-        a.add_values(rows, s);
+        a.add_values(values, s);
     }
     // the waves' parts, then the workgroup's
     const float l = column_sum(a.l);

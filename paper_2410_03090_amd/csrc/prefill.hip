@@ -11,11 +11,6 @@ namespace uncomp {
 
 namespace {
 
-struct Seq {
-    int64_t q0, k0;      // element offsets of the first query / key row (sequence stride included)
-    int nq, nk;
-};
-
 __device__ __forceinline__ void rows_of(const AttnRows& r, int s, int* first, int* n) {
     int f = r.first != nullptr ? r.first[s] : 0;
     f = f < 0 ? 0 : (f > r.rows ? r.rows : f);
@@ -28,9 +23,11 @@ __device__ __forceinline__ void rows_of(const AttnRows& r, int s, int* first, in
 // Work item number `rank` of the tiles of all sequences, those with most keys first (a workgroup that starts late then has little
 // to do; equal ones in order of their sequence).  A tile is `tile` columns; its keys are counted in blocks of 64.  The tiles of a
 // sequence see ever more keys, so how many see at least x blocks is a subtraction, and x is found by bisection, 64 sequences at a time.
-// Returns whether there is such a tile; called by whole waves, the same for all lanes.
+// Returns whether there is such a tile; called by whole waves, the same for all lanes.  blocks: those of all tiles (a tile sees
+// about the mean of its sequence's first and last), 0 with more than 64 sequences, which are taken in their order.
 struct Tile {
     int seq, tile, q_first, nq, k_first, nk;
+    int64_t blocks;
 };
 __device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile, int64_t rank, Tile* out) {
     const int lane = threadIdx.x & 63;
@@ -52,16 +49,27 @@ __device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile, int64_
         const int first = row <= 1 ? 0 : (int)((int64_t)(row - 1) * a.G / tile);
         return first < n ? n - first : 0;
     };
-    auto wave_total = [](int v) {
+    auto wave_total = [](auto v) {
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
         return v;
     };
     int qf, nq, kf, nk;
+    out->blocks = 0;
+    if (a.n_seq == 1) {                                    // nothing to look for: its last tile sees most
+        seq_of(0, &qf, &nq, &kf, &nk);
+        const int n = tiles_of(nq), first = max(0, min(nk, nk - nq + (tile - 1) / a.G + 1));
+        *out = Tile{0, n - 1 - (int)rank, qf, nq, kf, nk, (int64_t)n * (first + nk) / 128};
+        return rank < n;
+    }
     if (a.n_seq <= 64) {
         seq_of(lane, &qf, &nq, &kf, &nk);
         const int n = tiles_of(nq);
         if (rank >= wave_total(n)) return false;
+        if (a.n_split > 1) {
+            const int first = max(0, min(nk, nk - nq + (tile - 1) / a.G + 1));
+            out->blocks = wave_total((int64_t)n * (first + nk) / 128);
+        }
         int most = (nk + 63) / 64;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, 64));
@@ -114,74 +122,166 @@ __device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile, int64_
     return false;
 }
 
-constexpr int kWaveCols = 64;      // columns of a workgroup of the wave kernel: sixteen a wave
+constexpr int kWaveCols = 64;      // columns of a workgroup of the fp32 kernel: sixteen a wave
+
+// What a tile of columns sees, and the part of it that one workgroup takes.  Where few tiles, or a few long ones, would leave much of
+// the chip idle, tiles are cut into parts of whole blocks of 64 keys, each about the target-th of all blocks but no fewer than
+// kLeastBlocks: a part leaves its outputs in fp32, and joining them takes as long as about that many blocks (fp32: two).  One layer of 8
+// KV heads, 4 query heads each, uncut and cut (us): 1 query on 20000 keys 456 / 45, 64 on 8000 194 / 47, 512 on 16000 386 / 142, a prompt of
+// 3000 142 / 93; a prompt of 1024, in parts of 8 blocks 38 / 41.
+// Key numbers below are counted from the part's first.
+constexpr int kLeastBlocks = 12, kLeastBlocksF32 = 2;
+__host__ __device__ inline int parts_of(int64_t blocks, int64_t all_blocks, int target, int least, int most) {
+    int64_t share = (all_blocks + target - 1) / target;
+    share = share < least ? least : share;
+    const int64_t n = (blocks + share / 2) / share;                       // to the nearest: not a second round for a little more than a share
+    return n < 1 ? 1 : n > most ? most : (int)n;
+}
+struct Part {
+    int s, h, q_first, nq, last_col, c0;     // sequence, KV head, its rows, last column, the tile's first
+    int shift, keys;                         // first key of the part (of the sequence's), keys in it
+    int off;                                 // column of row i sees keys up to off + i
+    int n_parts;
+};
+// Workgroups are numbered by head first (eight KV heads are one per XCD, whose L2 then holds that head's rows alone), then by
+// tile, then by part, the last part first: what is cut starts before the short tiles, and those without a part are on every XCD.
+__device__ __forceinline__ bool find_part(const PrefillArgs& a, int tile, Part* p, int item, int part) {
+    const int h = item % a.H;
+    Tile w;
+    if (!find_tile(a, tile, item / a.H, &w)) return false;
+    const auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int nk = uniform(w.nk), nq = uniform(w.nq);
+    p->s = uniform(w.seq);
+    p->h = h;
+    p->q_first = uniform(w.q_first);
+    p->nq = nq;
+    p->last_col = nq * a.G - 1;
+    p->c0 = uniform(w.tile) * tile;
+    const int off = nk - nq, seen = min(nk, off + min(p->c0 + tile - 1, p->last_col) / a.G + 1);
+    const int blocks = seen <= 0 ? 0 : (seen + 63) / 64;
+    const int n = a.n_split == 1 ? 1 : parts_of(blocks, w.blocks * a.H, a.target, a.least, a.n_split);
+    const int per = (blocks + n - 1) / n;
+    p->n_parts = per == 0 ? 1 : (blocks + per - 1) / per;
+    p->shift = min(part * per, blocks) * 64;
+    p->keys = min(min(per, blocks - p->shift / 64) * 64, nk - p->shift);
+    p->off = off - p->shift;
+    p->shift += uniform(w.k_first);
+    return part < p->n_parts;
+}
+__device__ __forceinline__ bool find_part(const PrefillArgs& a, int tile, Part* p) {
+    return find_part(a, tile, p, blockIdx.x % a.items, a.n_split - 1 - blockIdx.x / a.items);
+}
+// where a part's unnormalised outputs and (maximum in base 2, sum) go
+__device__ __forceinline__ int64_t part_row(const PrefillArgs& a, int tile, int col) {
+    return ((int64_t)a.n_split * a.items - a.items - blockIdx.x + 2 * (blockIdx.x % a.items)) * tile + col;      // [part][item][column]
+}
 
 }  // namespace
 
-// Sixteen columns per wave, keys straight from memory.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void prefill_wave_kernel(PrefillArgs a) {
-    using A = WaveAttend<T, D, sizeof(T) == 4>;
+// ---- fp32 ------------------------------------------------------------------------------------------------------------
+// Sixteen columns per wave, rows straight from memory into the operands: the fp32 matrix cores take 2048 cycles for sixteen rows of
+// 128 features, which no fetch through the caches outlasts.  The next block's keys are on their way from the moment this one's
+// logits are there, the values from the block's start.
+template <int D>
+__global__ __launch_bounds__(256) void prefill_f32_kernel(PrefillArgs a) {
+    using A = WaveAttend<float, D>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4;
-    const int G = a.G;
     const float scale2 = kLog2eA * (D == 128 ? 0.08838834764831845f : 0.125f);
-    const int h = blockIdx.x % a.H;
-    Tile w;
-    if (!find_tile(a, kWaveCols, blockIdx.x / a.H, &w)) return;
-    const int s = w.seq, q_first = w.q_first, nq = w.nq, k_first = w.k_first, nk = w.nk;
-    const int off = nk - nq;
-    const int c0 = w.tile * kWaveCols + 16 * wave, last_col = nq * G - 1;
-    if (c0 > last_col) return;
-    const int col = c0 + (lane & 15), cc = col > last_col ? last_col : col;
-    const int qi = cc / G, head = h * G + cc % G;
-    const int lim = off + qi;                                         // last key this column sees
-    const int all = off + c0 / G;                                     // keys up to here are seen by every column
-    const int end = min(nk, off + min(c0 + 15, last_col) / G + 1);
-    const T* Q = static_cast<const T*>(a.Q) + s * a.q.ss + head * a.q.sh + (int64_t)(q_first + qi) * a.q.sr;
-    const T* K = static_cast<const T*>(a.K) + s * a.k.ss + h * a.k.sh + (int64_t)k_first * a.k.sr;
-    const T* V = static_cast<const T*>(a.V) + s * a.v.ss + h * a.v.sh + (int64_t)k_first * a.v.sr;
+    Part w;
+    if (!find_part(a, kWaveCols, &w)) return;
+    const int c0 = w.c0 + 16 * wave;
+    if (c0 > w.last_col) return;
+    const int col = c0 + (lane & 15), cc = min(col, w.last_col);
+    const int qi = cc / a.G, head = w.h * a.G + cc % a.G;
+    const int lim = min(w.off + qi, w.keys - 1);                          // last key the lane's column sees
+    const int all = min(w.off + c0 / a.G, w.keys - 1);                    // keys up to here are seen by every column
+    const int end = min(w.off + min(c0 + 15, w.last_col) / a.G + 1, w.keys);
+    const float* Q = static_cast<const float*>(a.Q) + w.s * a.q.ss + head * a.q.sh + (int64_t)(w.q_first + qi) * a.q.sr;
+    const float* K = static_cast<const float*>(a.K) + w.s * a.k.ss + w.h * a.k.sh + (int64_t)w.shift * a.k.sr;
+    const float* V = static_cast<const float*>(a.V) + w.s * a.v.ss + w.h * a.v.sh + (int64_t)w.shift * a.v.sr;
     A at;
     at.reset();
     at.load_query(Q, lane);
+    typename A::Keys keys;
+    typename A::Values values;
+    const auto fetch_keys = [&](int r0) { A::load_keys(keys, lane, [&](int r) { return K + min(r0 + r, w.keys - 1) * a.k.sr; }); };
+    if (end > 0) fetch_keys(0);
     for (int r0 = 0; r0 < end; r0 += A::kBlock) {
-        typename A::Rows rows;
+        A::load_values(values, lane, [&](int r) { return V + min(r0 + r, w.keys - 1) * a.v.sr; });
         float p[A::kPerLane];
-        A::load(rows, lane, [&](int r) { return K + min(r0 + r, nk - 1) * a.k.sr; }, [&](int r) { return V + min(r0 + r, nk - 1) * a.v.sr; });
-        at.logits(rows, scale2, p);
+        at.logits(keys, scale2, p);
+        fetch_keys(r0 + A::kBlock);
         if (r0 + A::kBlock - 1 <= all) {
             take_logits(at, p);
-            at.add_values(rows, p);
+            at.add_values(values, p);
         } else {
-            A::clear_values(rows, lane, nk - r0);
+            A::clear_values(values, lane, w.keys - r0);
 #pragma unroll
             for (int e = 0; e < A::kPerLane; ++e)
                 if (r0 + A::value_row(lane, e) > lim) p[e] = -INFINITY;
             take_logits(at, p);
-            add_masked_values(at, rows, p, lane, [&](int r) { return r0 + r <= lim; });
+            add_masked_values(at, values, p, lane, [&](int r) { return r0 + r <= lim; });
         }
     }
     const float l = column_sum(at.l);
-    if (col <= last_col) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        T* O = static_cast<T*>(a.out) + s * a.o.ss + head * a.o.sh + (int64_t)(q_first + qi) * a.o.sr;
+    if (col > w.last_col) return;
+    if (w.n_parts > 1) {
+        const int64_t row = part_row(a, kWaveCols, col - w.c0);
+        float* acc = a.part_acc + row * D;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int d = A::kVw * (4 * j + i);
-            if constexpr (sizeof(T) == 2) {
-                typedef __bf16 out_t __attribute__((ext_vector_type(A::kVw)));
-                out_t v;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int t2 = 0; t2 < A::kVw; ++t2) v[t2] = (__bf16)(at.o[t2][i] * inv);
-                *reinterpret_cast<out_t*>(O + d) = v;
-            } else {
+            for (int t = 0; t < A::kVw; t += 4)
+                *reinterpret_cast<f32x4_t*>(acc + A::kVw * (4 * j + i) + t) = f32x4_t{at.o[t][i], at.o[t + 1][i], at.o[t + 2][i], at.o[t + 3][i]};
+        if (j == 0) a.part_ml[row] = make_float2(at.m, l);
+        return;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    float* O = static_cast<float*>(a.out) + w.s * a.o.ss + head * a.o.sh + (int64_t)(w.q_first + qi) * a.o.sr;
 #pragma unroll
-                for (int t2 = 0; t2 < A::kVw; t2 += 4)
-                    *reinterpret_cast<f32x4_t*>(O + d + t2) =
-                        f32x4_t{at.o[t2][i] * inv, at.o[t2 + 1][i] * inv, at.o[t2 + 2][i] * inv, at.o[t2 + 3][i] * inv};
-            }
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t < A::kVw; t += 4)
+            *reinterpret_cast<f32x4_t*>(O + A::kVw * (4 * j + i) + t) =
+                f32x4_t{at.o[t][i] * inv, at.o[t + 1][i] * inv, at.o[t + 2][i] * inv, at.o[t + 3][i] * inv};
+    if (a.lse != nullptr && j == 0)
+        a.lse[w.s * a.lse_ss + head * a.lse_sh + w.q_first + qi] = l == 0.f ? -INFINITY : (at.m + log2f(l)) * kLn2A;
+}
+
+// Joins the parts of a tile's columns, sixteen columns a workgroup, four features a lane.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void prefill_join_kernel(PrefillArgs a, int tile) {
+    constexpr int kLanes = D / 4, kPer = 256 / kLanes;
+    const int groups = tile / 16, item = blockIdx.x / groups;
+    Part w;
+    if (!find_part(a, tile, &w, item, 0) || w.n_parts == 1) return;
+    for (int i = threadIdx.x / kLanes; i < 16; i += kPer) {
+        const int in_tile = (blockIdx.x % groups) * 16 + i, col = w.c0 + in_tile, d = (threadIdx.x % kLanes) * 4;
+        if (col > w.last_col) continue;
+        const int64_t row = (int64_t)item * tile + in_tile, next = (int64_t)a.items * tile;
+        float m = -INFINITY;
+        for (int p = 0; p < w.n_parts; ++p) m = fmaxf(m, a.part_ml[row + p * next].x);
+        float l = 0.f;
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < w.n_parts; ++p) {
+            const float2 ml = a.part_ml[row + p * next];
+            const f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.part_acc + (row + p * next) * D + d);
+            const float f = __builtin_amdgcn_exp2f(ml.x - reference(m));
+            l = fmaf(f, ml.y, l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = ml.y == 0.f ? o[e] : fmaf(f, v[e], o[e]);
         }
-        if (a.lse != nullptr && j == 0)
-            a.lse[s * a.lse_ss + head * a.lse_sh + q_first + qi] = l == 0.f ? -INFINITY : (at.m + log2f(l)) * kLn2A;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int qi = col / a.G, head = w.h * a.G + col % a.G;
+        T* O = static_cast<T*>(a.out) + w.s * a.o.ss + head * a.o.sh + (int64_t)(w.q_first + qi) * a.o.sr + d;
+        if constexpr (sizeof(T) == 2) {
+            typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<bf16x4_t*>(O) = bf16x4_t{(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv), (__bf16)(o[3] * inv)};
+        } else {
+            *reinterpret_cast<f32x4_t*>(O) = o * inv;
+        }
+        if (a.lse != nullptr && d == 0)
+            a.lse[w.s * a.lse_ss + head * a.lse_sh + w.q_first + qi] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2A;
     }
 }
 
@@ -225,24 +325,20 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
     __shared__ __align__(16) unsigned char lds[2][2][kTileBytes];        // [buffer][keys, values]
     __shared__ int not_finite[2];                                         // tile (from one) in the buffer whose values are not all finite
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, c = lane & 31;
-    const int G = a.G, h = blockIdx.x % a.H;
-    Tile w;
-    if (!find_tile(a, kCols, blockIdx.x / a.H, &w)) return;
-    const int nk = __builtin_amdgcn_readfirstlane(w.nk), nq = __builtin_amdgcn_readfirstlane(w.nq), s = __builtin_amdgcn_readfirstlane(w.seq);
-    const int off = nk - nq, last_col = nq * G - 1;
-    const int c_wg = __builtin_amdgcn_readfirstlane(w.tile) * kCols, c_wave = c_wg + 32 * wave;
-    const int col = c_wave + c, cc = min(col, last_col);
-    const int qi = cc / G, head = h * G + cc % G;
-    const int lim = off + qi;                                             // last key the lane's column sees
-    const int wave_end = min(nk, off + min(c_wave + 31, last_col) / G + 1);      // keys that any of the wave's columns sees
-    const int wg_all = off + c_wg / G, wg_end = min(nk, off + min(c_wg + kCols - 1, last_col) / G + 1);
-    const int n_tiles = wg_end <= 0 ? 0 : (wg_end + kTileKeys - 1) / kTileKeys;
-    const int n_whole = wg_all < 0 ? 0 : min(nk, wg_all + 1) / kTileKeys;            // tiles that all columns see all of
+    const int G = a.G;
+    Part w;
+    if (!find_part(a, kCols, &w)) return;
+    const int c_wave = w.c0 + 32 * wave, col = c_wave + c, cc = min(col, w.last_col);
+    const int qi = cc / G, head = w.h * G + cc % G, nk = w.keys;
+    const int lim = min(w.off + qi, nk - 1);                              // last key the lane's column sees
+    const int wave_end = min(nk, w.off + min(c_wave + 31, w.last_col) / G + 1);      // keys that any of the wave's columns sees
+    const int wg_all = min(w.off + w.c0 / G, nk - 1);
+    const int n_tiles = nk <= 0 ? 0 : (nk + kTileKeys - 1) / kTileKeys;
+    const int n_whole = wg_all < 0 ? 0 : (wg_all + 1) / kTileKeys;        // tiles that all columns see all of
     const float scale2 = kLog2eA * (D == 128 ? 0.08838834764831845f : 0.125f);
-    const int q_first = __builtin_amdgcn_readfirstlane(w.q_first), k_first = __builtin_amdgcn_readfirstlane(w.k_first);
-    const bf16_bits* Q = static_cast<const bf16_bits*>(a.Q) + s * a.q.ss + head * a.q.sh + (int64_t)(q_first + qi) * a.q.sr;
-    const bf16_bits* K = static_cast<const bf16_bits*>(a.K) + s * a.k.ss + h * a.k.sh + (int64_t)k_first * a.k.sr;
-    const bf16_bits* V = static_cast<const bf16_bits*>(a.V) + s * a.v.ss + h * a.v.sh + (int64_t)k_first * a.v.sr;
+    const bf16_bits* Q = static_cast<const bf16_bits*>(a.Q) + w.s * a.q.ss + head * a.q.sh + (int64_t)(w.q_first + qi) * a.q.sr;
+    const bf16_bits* K = static_cast<const bf16_bits*>(a.K) + w.s * a.k.ss + w.h * a.k.sh + (int64_t)w.shift * a.k.sr;
+    const bf16_bits* V = static_cast<const bf16_bits*>(a.V) + w.s * a.v.ss + w.h * a.v.sh + (int64_t)w.shift * a.v.sr;
 
     bf16x8_t q[kSteps];
 #pragma unroll
@@ -440,56 +536,107 @@ __global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a)
     }
     const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(other[0]) + __uint_as_float(other[1]);
-    if (col <= last_col) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        bf16_bits* O = static_cast<bf16_bits*>(a.out) + s * a.o.ss + head * a.o.sh + (int64_t)(q_first + qi) * a.o.sr;
-        typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+    if (col > w.last_col) return;
+    if (w.n_parts > 1) {
+        const int64_t row = part_row(a, kCols, col - w.c0);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                bf16x4_t v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[b][r + e] * inv);
-                *reinterpret_cast<bf16x4_t*>(O + 32 * b + 2 * r + 4 * half) = v;
-            }
-        if (a.lse != nullptr && half == 0)
-            a.lse[s * a.lse_ss + head * a.lse_sh + q_first + qi] = l == 0.f ? -INFINITY : (m * scale2 + log2f(l)) * kLn2A;
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<f32x4_t*>(a.part_acc + row * D + 32 * b + 2 * r + 4 * half) = f32x4_t{o[b][r], o[b][r + 1], o[b][r + 2], o[b][r + 3]};
+        if (half == 0) a.part_ml[row] = make_float2(m * scale2, l);
+        return;
     }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    bf16_bits* O = static_cast<bf16_bits*>(a.out) + w.s * a.o.ss + head * a.o.sh + (int64_t)(w.q_first + qi) * a.o.sr;
+    typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            bf16x4_t v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[b][r + e] * inv);
+            *reinterpret_cast<bf16x4_t*>(O + 32 * b + 2 * r + 4 * half) = v;
+        }
+    if (a.lse != nullptr && half == 0)
+        a.lse[w.s * a.lse_ss + head * a.lse_sh + w.q_first + qi] = l == 0.f ? -INFINITY : (m * scale2 + log2f(l)) * kLn2A;
 }
 
-size_t prefill_attention_bytes(int, int, int, int, int, int) { return 0; }
+// ---- host ------------------------------------------------------------------------------------------------------------
+namespace {
+struct Plan {
+    int tile;            // columns of a workgroup
+    int n_split, target, least;
+    int64_t items;       // tiles of all KV heads, at most
+    size_t acc_off, bytes;
+};
+// 64-wide heads take tiles of 128 columns, two workgroups a CU: as much work for the vector unit comes with half the products, and
+// two that do not wait for each other fill it better (8 KV heads of 1024 rows 28.5 -> 22.3 us, 8192 rows 357 -> 347).
+Plan plan(bool f32, bool packed, int n_seq, int H, int G, int D, int q_rows, int k_rows) {
+    const int64_t cols = (int64_t)q_rows * G;
+    Plan p;
+    p.tile = f32 ? kWaveCols : D == 64 ? 128 : 256;
+    p.target = p.tile == 256 ? 256 : 512;                                 // workgroups that run at a time
+    p.least = f32 ? kLeastBlocksF32 : kLeastBlocks;
+    // most tiles that the sequences can have: whole ones, and one broken one each
+    p.items = (packed ? cols / p.tile + n_seq : (cols + p.tile - 1) / p.tile * n_seq) * H;
+    // as if the rows were one sequence's; how they are divided only the device knows
+    const int64_t most = ((int64_t)k_rows + 63) / 64, first = (k_rows > q_rows ? (int64_t)k_rows - q_rows : 0) / 64;
+    p.n_split = n_seq > 64 ? 1 : parts_of(most, p.items * (first + most + 1) / 2, p.target, p.least, 64);
+    p.acc_off = align_up((size_t)p.items * p.n_split * p.tile * sizeof(float2), 256);
+    p.bytes = p.n_split == 1 ? 0 : p.acc_off + (size_t)p.items * p.n_split * p.tile * D * sizeof(float);
+    return p;
+}
+}  // namespace
+
+size_t prefill_attention_bytes(int n_seq, int H, int G, int D, int q_rows, int k_rows) {
+    size_t most = 0;
+    for (int i = 0; i < 4; ++i) {
+        const size_t b = plan(i & 1, i & 2, n_seq, H, G, D, q_rows, k_rows).bytes;
+        most = b > most ? b : most;
+    }
+    return most;
+}
+
+bool prefill_attention_fits(const PrefillArgs& a, uncomp_dtype dt, int D) {
+    return plan(dt == UNCOMP_F32, a.q.first != nullptr, a.n_seq, a.H, a.G, D, a.q.rows, a.k.rows).items <= (1 << 30) / 16;
+}
 
 namespace {
-// most tiles that the sequences can have: whole ones, and one broken one each
-int64_t most_tiles(const PrefillArgs& a, int tile) {
-    const int64_t cols = (int64_t)a.q.rows * a.G;
-    return a.q.first != nullptr ? cols / tile + a.n_seq : (cols + tile - 1) / tile * a.n_seq;
-}
-template <int D, int NW>
-hipError_t prefill_tiles(const PrefillArgs& a, const Env& env) {
-    env.begin("prefill_tile");
-    prefill_tile_kernel<D, NW><<<(unsigned)(most_tiles(a, 32 * NW) * a.H), 64 * NW, 0, env.s>>>(a);
-    env.end();
-    return hipGetLastError();
-}
-template <typename T, int D>
-hipError_t prefill_of(const PrefillArgs& a, const Env& env) {
-    if constexpr (sizeof(T) == 2) {
-        const bool near = a.k.sr < 1 << 22 && a.v.sr < 1 << 22;      // 64 rows span less than 2 GiB
-        if (near && !env.force_alu) return prefill_tiles<D, 8>(a, env);
+template <int D>
+hipError_t prefill_of(PrefillArgs a, bool f32, char* ws, size_t ws_bytes, const Env& env) {
+    Plan p = plan(f32, a.q.first != nullptr, a.n_seq, a.H, a.G, D, a.q.rows, a.k.rows);
+    if (p.bytes > ws_bytes) p.n_split = 1;                               // no room for parts: whole tiles
+    a.n_split = p.n_split;
+    a.target = p.target;
+    a.least = p.least;
+    a.items = (unsigned)p.items;
+    a.part_ml = reinterpret_cast<float2*>(ws);
+    a.part_acc = reinterpret_cast<float*>(ws + p.acc_off);
+    const unsigned grid = (unsigned)(p.items * p.n_split);
+    if (f32) {
+        env.begin("prefill_f32");
+        prefill_f32_kernel<D><<<grid, 256, 0, env.s>>>(a);
+        env.end();
+    } else {
+        env.begin("prefill_tile");
+        constexpr int kWaves = D == 64 ? 4 : 8;
+        prefill_tile_kernel<D, kWaves><<<grid, 64 * kWaves, 0, env.s>>>(a);
+        env.end();
     }
-    const int64_t grid = most_tiles(a, kWaveCols) * a.H;
-    env.begin("prefill_wave");
-    prefill_wave_kernel<T, D><<<(unsigned)grid, 256, 0, env.s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.n_split == 1) return e;
+    env.begin("prefill_join");
+    if (f32) prefill_join_kernel<float, D><<<(unsigned)(p.items * p.tile / 16), 256, 0, env.s>>>(a, p.tile);
+    else prefill_join_kernel<bf16_bits, D><<<(unsigned)(p.items * p.tile / 16), 256, 0, env.s>>>(a, p.tile);
     env.end();
     return hipGetLastError();
 }
 }  // namespace
 
-hipError_t launch_prefill_attention(const PrefillArgs& a, uncomp_dtype dt, int D, char*, size_t, const Env& env) {
-    if (dt == UNCOMP_BF16) return D == 128 ? prefill_of<bf16_bits, 128>(a, env) : prefill_of<bf16_bits, 64>(a, env);
-    return D == 128 ? prefill_of<float, 128>(a, env) : prefill_of<float, 64>(a, env);
+hipError_t launch_prefill_attention(const PrefillArgs& a, uncomp_dtype dt, int D, char* ws, size_t ws_bytes, const Env& env) {
+    return D == 128 ? prefill_of<128>(a, dt == UNCOMP_F32, ws, ws_bytes, env) : prefill_of<64>(a, dt == UNCOMP_F32, ws, ws_bytes, env);
 }
 
 }  // namespace uncomp
