@@ -49,6 +49,7 @@ uncomp_status uncomp_create(uncomp_ctx** ctx_out, int device, size_t workspace_b
     if (e == hipSuccess) e = init_select_kernels();
     if (e == hipSuccess) e = init_jacobi_kernels();
     if (e == hipSuccess) e = init_decode_kernels();
+    if (e == hipSuccess) e = init_paged_kernels();
     if (e == hipSuccess) e = init_subspace_kernels();
     if (e == hipSuccess) e = hipStreamCreateWithFlags(&ctx->side, hipStreamNonBlocking);
     // zero before the first call, which may come on any stream; cleared on a stream that waits for no other work

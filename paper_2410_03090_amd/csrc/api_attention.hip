@@ -177,7 +177,7 @@ uncomp_status uncomp_paged_step(uncomp_ctx* ctx, const uncomp_paged_cache* cache
     if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned4(pos) || !aligned4(out))
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: 16-byte aligned q, k_new and v_new required", who);
     const int rows = c.max_pages << c.shift;
-    if ((int64_t)c.n_heads * (((int64_t)rows + 1023) / 1024) > 0x7fffffffLL) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
+    if ((int64_t)c.n_heads * (rows / 256 + 64) > 0x7fffffffLL) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
     const PagedStepPlan p = plan_paged_step(c.n_heads, G, cache->D, rows);
     st = take_workspace(ctx, who, p.bytes, stream);
     if (st != UNCOMP_OK) return st;

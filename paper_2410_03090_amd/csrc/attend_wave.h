@@ -3,11 +3,12 @@
 // crosses lanes but the maximum:
 //
 //   logits    S^T = K Q^T: lane (c = lane % 16, j = lane / 16) ends up with column c of four consecutive rows of every tile.
-//             Which key is which row of a tile is free: they are dealt out so that lane group j holds keys 8 j ... 8 j + 7
-//             of a block of 32 (fp32: 4 j ... 4 j + 3 of 16).
+//             Which key is which row of a tile is free: register e of lane group j is key 4 e + j of a tile of sixteen.
 //   weights   p = 2^(s - m): what the lane holds is its operand of the second product as it is.
-//   output    O^T = V^T P^T: the lane loads features c D / 16 ... of its own eight (four) value rows and pairs the bf16 of two
-//             rows up by byte permutes; the t-th product yields the features D / 16 * i + t, i = 0 ... 15.
+//   output    O^T = V^T P^T: the lane loads features c D / 16 ... of its own eight (four) value rows, so that one load is four whole
+//             rows behind one another, and pairs the bf16 of two rows up by byte permutes; the t-th product yields the features
+//             D / 16 * i + t, i = 0 ... 15.  (With keys 8 j + e of 32 instead, a load is four rows 2 KB apart, which are in two of the
+//             sixteen channels of the cache.)
 //
 // Outputs are fp32, so bf16 weights are the sum of three bf16: twice the upper half of what is left of a float, shrunk a little
 // first so that no term is zero (zero times an infinite value is NaN, the weight times it is infinite), then the rest, which
@@ -56,6 +57,9 @@ __device__ __forceinline__ Words<N> load_words(const void* p) {
     return r;
 }
 
+// row of a tile that register e of lane group j holds
+__device__ __forceinline__ int row_of(int e, int j) { return 4 * e + j; }
+
 template <typename T, int D>
 struct WaveAttend;
 
@@ -83,22 +87,38 @@ struct WaveAttend<bf16_bits, D> {
             q[s] = __builtin_bit_cast(bf16x8_t, w);
         }
     }
-    static __device__ __forceinline__ int key_row(int lane, int tile) { return 8 * ((lane & 15) >> 2) + 4 * tile + (lane & 3); }
-    static __device__ __forceinline__ int value_row(int lane, int e) { return 8 * (lane >> 4) + e; }
-    // row (of the block) -> the row's address
-    template <typename F>
-    static __device__ __forceinline__ void load_keys(Keys& k, int lane, F&& row) {
+    static __device__ __forceinline__ int key_row(int lane, int tile) { return 16 * tile + row_of(lane & 3, (lane & 15) >> 2); }
+    static __device__ __forceinline__ int value_row(int lane, int e) { return 16 * (e >> 2) + row_of(e & 3, lane >> 4); }
+    // tile0, tile1: the first rows of the block's two tiles
+    static __device__ __forceinline__ void load_keys(Keys& k, int lane, const bf16_bits* tile0, const bf16_bits* tile1) {
+        const int at = key_row(lane, 0) * D + 8 * (lane >> 4);
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-            const bf16_bits* p = row(key_row(lane, a));
+        for (int a = 0; a < 2; ++a)
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) k.w[a][s] = load_words<4>(p + 32 * s + 8 * (lane >> 4));
+            for (int s = 0; s < kSteps; ++s) k.w[a][s] = load_words<4>((a ? tile1 : tile0) + (at + 32 * s));
+    }
+    static __device__ __forceinline__ void load_values(Values& v, int lane, const bf16_bits* tile0, const bf16_bits* tile1) {
+        const int at = value_row(lane, 0) * D + kVw * (lane & 15);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.w[e] = load_words<kVw / 2>((e < 4 ? tile0 : tile1) + (at + 4 * (e & 3) * D));
+    }
+    // one row in another's place, in the lanes that hold it: row `at` of the block
+    static __device__ __forceinline__ void put_key(Keys& k, int lane, int at, const bf16_bits* row) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const Words<4> w = load_words<4>(row + 32 * s + 8 * (lane >> 4));
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) k.w[a][s].w[i] = key_row(lane, a) == at ? w.w[i] : k.w[a][s].w[i];
         }
     }
-    template <typename F>
-    static __device__ __forceinline__ void load_values(Values& v, int lane, F&& row) {
+    static __device__ __forceinline__ void put_value(Values& v, int lane, int at, const bf16_bits* row) {
+        const Words<kVw / 2> w = load_words<kVw / 2>(row + kVw * (lane & 15));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v.w[e] = load_words<kVw / 2>(row(value_row(lane, e)) + kVw * (lane & 15));
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int i = 0; i < kVw / 2; ++i) v.w[e].w[i] = value_row(lane, e) == at ? w.w[i] : v.w[e].w[i];
     }
     static __device__ __forceinline__ void clear_value(Values& v, int e) {
 #pragma unroll
@@ -163,21 +183,40 @@ struct WaveAttend<float, D> {
         for (int s = 0; s < kSteps; ++s)
             q[s] = qrow != nullptr ? *reinterpret_cast<const f32x4_t*>(qrow + 16 * s + 4 * (lane >> 4)) : f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    static __device__ __forceinline__ int key_row(int lane, int) { return lane & 15; }
-    static __device__ __forceinline__ int value_row(int lane, int e) { return 4 * (lane >> 4) + e; }
-    template <typename F>
-    static __device__ __forceinline__ void load_keys(Keys& k, int lane, F&& row) {
-        const float* p = row(key_row(lane, 0));
+    static __device__ __forceinline__ int key_row(int lane, int) { return row_of(lane & 3, (lane & 15) >> 2); }
+    static __device__ __forceinline__ int value_row(int lane, int e) { return row_of(e, lane >> 4); }
+    static __device__ __forceinline__ void load_key(Keys& k, int lane, const float* row) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) k.w[s] = *reinterpret_cast<const f32x4_t*>(p + 16 * s + 4 * (lane >> 4));
+        for (int s = 0; s < kSteps; ++s) k.w[s] = *reinterpret_cast<const f32x4_t*>(row + 16 * s + 4 * (lane >> 4));
     }
-    template <typename F>
-    static __device__ __forceinline__ void load_values(Values& v, int lane, F&& row) {
+    static __device__ __forceinline__ void load_keys(Keys& k, int lane, const float* tile0, const float*) {
+        load_key(k, lane, tile0 + key_row(lane, 0) * D);
+    }
+    // e: which of the lane's rows
+    static __device__ __forceinline__ void load_value(Values& v, int lane, int e, const float* row) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float* p = row(value_row(lane, e)) + kVw * (lane & 15);
+        for (int i = 0; i < kVw / 4; ++i) v.w[e][i] = *reinterpret_cast<const f32x4_t*>(row + kVw * (lane & 15) + 4 * i);
+    }
+    static __device__ __forceinline__ void load_values(Values& v, int lane, const float* tile0, const float*) {
 #pragma unroll
-            for (int i = 0; i < kVw / 4; ++i) v.w[e][i] = *reinterpret_cast<const f32x4_t*>(p + 4 * i);
+        for (int e = 0; e < 4; ++e) load_value(v, lane, e, tile0 + value_row(lane, e) * D);
+    }
+    static __device__ __forceinline__ void put_key(Keys& k, int lane, int at, const float* row) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const f32x4_t w = *reinterpret_cast<const f32x4_t*>(row + 16 * s + 4 * (lane >> 4));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k.w[s][i] = key_row(lane, 0) == at ? w[i] : k.w[s][i];
+        }
+    }
+    static __device__ __forceinline__ void put_value(Values& v, int lane, int at, const float* row) {
+#pragma unroll
+        for (int i = 0; i < kVw / 4; ++i) {
+            const f32x4_t w = *reinterpret_cast<const f32x4_t*>(row + kVw * (lane & 15) + 4 * i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v.w[e][i][x] = value_row(lane, e) == at ? w[x] : v.w[e][i][x];
         }
     }
     // value rows from n on are zeros (what lies there is nobody's)
@@ -217,14 +256,17 @@ struct WaveAttend<float, D> {
     }
 };
 
-// The running maximum takes a block's logits in: s becomes the weights, sums and outputs are brought to the new reference.
+// The running maximum takes a block's logits in: s becomes the weights, sums and outputs are brought to the new reference.  That
+// follows the maximum when it has grown by more than a factor of 2^8 of the weights: until then they are at most 2^8, which
+// floats hold as precisely as what is below one.
 template <typename A>
 __device__ __forceinline__ void take_logits(A& a, float (&s)[A::kPerLane]) {
     float top = s[0];
 #pragma unroll
     for (int e = 1; e < A::kPerLane; ++e) top = fmaxf(top, s[e]);
-    const float m_new = fmaxf(a.m, column_max(top));
-    if (__any(m_new != a.m)) {
+    top = column_max(top);
+    if (__any(top > a.m + 8.f)) {
+        const float m_new = fmaxf(a.m, top);
         const float f = __builtin_amdgcn_exp2f(a.m - reference(m_new));
         a.l *= f;
 #pragma unroll
@@ -264,7 +306,7 @@ __device__ __forceinline__ void add_masked_values(A& a, const typename A::Values
 #pragma unroll
         for (int t = 0; t < A::kVw; ++t) before[t] = a.o[t];
         a.add_values(one, pe);
-        const bool seen = sees(row);
+        const bool seen = sees(row_of(e, row / A::kPerLane));
 #pragma unroll
         for (int t = 0; t < A::kVw; ++t)
 #pragma unroll

@@ -271,12 +271,13 @@ struct PagedCache {
     int n_heads, n_pages, shift, max_pages;
 };
 struct PagedStepPlan {
-    int n_split;         // parts per head
+    bool one_launch;     // a workgroup per head, nothing in the workspace
+    int n_split;         // parts of all heads together, but for one broken one of each
     int rows;            // rows a head's table has room for
-    size_t head_off;     // int2  [n_heads]: rows before and after
-    size_t ml_off;       // float [n_heads][n_split][G][2]
-    size_t acc_off;      // float [n_heads][n_split][G][D]
-    size_t logit_off;    // float [n_heads][rows][G]
+    size_t head_off;     // int4  [n_heads]: rows before and after, first part, parts
+    size_t ml_off;       // float2 [n_split + n_heads][G]
+    size_t acc_off;      // float [n_split + n_heads][G][D]
+    size_t logit_off;    // float [n_heads][query heads, rounded up to 4, 8 or 16][rows]
     size_t bytes;
 };
 PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows);
@@ -339,6 +340,7 @@ hipError_t init_select_kernels();
 hipError_t init_score_kernels();
 hipError_t init_jacobi_kernels();
 hipError_t init_decode_kernels();
+hipError_t init_paged_kernels();
 hipError_t init_subspace_kernels();
 // Largest dynamic LDS request of the bf16 decode update kernel (three tables of [np_max][GT] floats; its early form takes
 // one, and 8 KB of its own).  The interface refuses caches beyond 64 KiB of them whichever form would run.

@@ -13,6 +13,10 @@ namespace {
 
 constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / 64;
 constexpr int kFinishThreads = 256, kFinishRows = 1024;
+constexpr int kSplitAim = 768;                        // workgroups of the attention of few heads: three a CU
+// One workgroup a head: from as many heads on as fill the chip, with logits that leave room for two workgroups on a CU.
+constexpr int kHeadLaunchHeads = 512;
+constexpr size_t kHeadLaunchLds = 76 * 1024;
 constexpr int kSelectThreads = 1024;
 
 __device__ __forceinline__ int head_rows(const PagedCache& c, int h) {
@@ -86,163 +90,409 @@ __global__ __launch_bounds__(256) void paged_copy_kernel(PagedCache c, const cha
 }
 
 // ---- one token -------------------------------------------------------------------------------------------------------
-// One part of one head's rows per workgroup, its blocks dealt to the waves in turn.  Leaves the part's maximum, sum and output
-// (joined by the finishing kernel) and every row's logits.
-template <typename T, int D>
-__global__ __launch_bounds__(kAttendThreads) void paged_attend_kernel(PagedCache c, const T* __restrict__ q, const T* __restrict__ k_new,
-                                                                      const T* __restrict__ v_new, int G, int n_split, PagedStepPlan p, char* ws) {
+namespace {
+
+// What the queries of one head attend to: its rows and, where it joins, the new token behind them.
+struct HeadRows {
+    int n, n1;
+    bool joins;
+};
+__device__ __forceinline__ HeadRows rows_of_head(const PagedCache& c, int h, bool has_new) {
+    HeadRows r;
+    r.n = head_rows(c, h);
+    r.joins = has_new && r.n < (c.max_pages << c.shift) &&
+              page_ok(c, c.table[(int64_t)h * c.max_pages + min(r.n >> c.shift, c.max_pages - 1)]);
+    r.n1 = r.n + (r.joins ? 1 : 0);
+    return r;
+}
+
+// One wave's share of a head: whole blocks of rows from `first` on, `step` rows apart, up to `end`, and the block of the head's last rows if
+// it falls to this wave (tail).  keep(row, logits): the lane's column's logits of its rows of the block that begins with `row`, in base 2.
+// A block's keys are on their way from the time the logits of the one before are there, its values from the time that one's have
+// been added, its pages two blocks ahead.
+template <typename T, int D, typename F>
+__device__ __forceinline__ void attend_rows(WaveAttend<T, D>& a, const PagedCache& c, int h, const HeadRows& hr, const T* kn, const T* vn, int first,
+                                            int step, int end, bool tail, int lane, F&& keep) {
     using A = WaveAttend<T, D>;
-    constexpr int kVw = A::kVw;
-    __shared__ float o_s[kAttendWaves][16][D];
-    __shared__ float ml_s[kAttendWaves][16][2];
-    const int h = blockIdx.x / n_split, part = blockIdx.x % n_split;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, j = lane >> 4;
-    const int n = head_rows(c, h), cap = c.max_pages << c.shift;
-    const bool joins = k_new != nullptr && n < cap && pool_row(c, h, n) >= 0;
-    const int n1 = n + (joins ? 1 : 0);
-    constexpr int kStep = A::kBlock * kAttendWaves;
-    const int chunk = ((n1 + n_split - 1) / n_split + kStep - 1) / kStep * kStep;
-    const int64_t begin64 = (int64_t)part * chunk;
-    const int begin = begin64 > n1 ? n1 : (int)begin64, end = min(n1, begin + chunk);
+    const float scale2 = kLog2eA * (D == 128 ? 0.08838834764831845f : 0.125f);
     const int32_t* table = c.table + (int64_t)h * c.max_pages;
     const T* K = static_cast<const T*>(c.K);
     const T* V = static_cast<const T*>(c.V);
+    const int in_page = (1 << c.shift) - 1, last = c.max_pages - 1;
+    // the pages of a block's two tiles (the same one unless pages hold sixteen rows); the pool's first is read in the place of one that is none
+    struct Pages {
+        int id[2];
+        __device__ __forceinline__ bool ok(const PagedCache& c, int tile) const { return page_ok(c, id[tile]); }
+    };
+    const auto pages_of = [&](int r0) __attribute__((always_inline)) {
+        Pages p;
+        p.id[0] = table[min(r0 >> c.shift, last)];
+        p.id[1] = A::kBlock > 16 && c.shift == 4 ? table[min((r0 >> 4) + 1, last)] : p.id[0];
+        return p;
+    };
+    const auto tile_at = [&](const T* pool, const Pages& p, int r0, int tile) __attribute__((always_inline)) {
+        return pool + (((int64_t)(p.ok(c, tile) ? p.id[tile] : 0) << c.shift) + ((r0 + 16 * tile) & in_page)) * D;
+    };
+    typename A::Keys keys;
+    typename A::Values values;
+    const auto load_keys = [&](const Pages& p, int r0) __attribute__((always_inline)) { A::load_keys(keys, lane, tile_at(K, p, r0, 0), tile_at(K, p, r0, 1)); };
+    const auto load_values = [&](const Pages& p, int r0) __attribute__((always_inline)) {
+        A::load_values(values, lane, tile_at(V, p, r0, 0), tile_at(V, p, r0, 1));
+    };
+    const auto block = [&](int r0, float (&s)[A::kPerLane]) __attribute__((always_inline)) {
+        keep(r0, s);
+        take_logits(a, s);
+        a.add_values(values, s);
+    };
+    if (tail) {
+        const int r0 = hr.n / A::kBlock * A::kBlock;
+        const Pages p = pages_of(r0);
+        load_keys(p, r0);
+        load_values(p, r0);
+        if (hr.joins) {
+            A::put_key(keys, lane, hr.n - r0, kn);
+            A::put_value(values, lane, hr.n - r0, vn);
+        }
+        float s[A::kPerLane];
+        a.logits(keys, scale2, s);
+#pragma unroll
+        for (int e = 0; e < A::kPerLane; ++e) {
+            const int r = r0 + A::value_row(lane, e);
+            const bool has = (r < hr.n && p.ok(c, e >> 2)) || (hr.joins && r == hr.n);
+            s[e] = has ? s[e] : -INFINITY;
+            if (!has) A::clear_value(values, e);
+        }
+        block(r0, s);
+    }
+    if (first >= end) return;
+    Pages p = pages_of(first), next = pages_of(first + step);
+    load_keys(p, first);
+    load_values(p, first);
+    for (int r0 = first; r0 < end; r0 += step) {
+        float s[A::kPerLane];
+        a.logits(keys, scale2, s);
+        // (behind the last block the loads are those of some page: nobody reads what they bring)
+        load_keys(next, r0 + step);
+        if (!p.ok(c, 0) || !p.ok(c, 1))
+#pragma unroll
+            for (int e = 0; e < A::kPerLane; ++e)
+                if (!p.ok(c, e >> 2)) {
+                    s[e] = -INFINITY;
+                    A::clear_value(values, e);
+                }
+        block(r0, s);
+        load_values(next, r0 + step);
+        p = next;
+        next = pages_of(r0 + 2 * step);
+    }
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void write_new_row(const PagedCache& c, int h, int n, const T* kn, const T* vn, const int32_t* pos, int threads) {
+    constexpr int kPieces = D * sizeof(T) / 16;
+    const int64_t at = pool_row(c, h, n);
+    const int t = threadIdx.x % threads;
+    if (t < kPieces) reinterpret_cast<uint4*>(static_cast<T*>(c.K) + at * D)[t] = reinterpret_cast<const uint4*>(kn)[t];
+    else if (t < 2 * kPieces) reinterpret_cast<uint4*>(static_cast<T*>(c.V) + at * D)[t - kPieces] = reinterpret_cast<const uint4*>(vn)[t - kPieces];
+    if (t == 0) {
+        c.idx[at] = pos[h];
+        c.len[h] = n + 1;
+    }
+}
+
+// Logits lie query head by query head, `stride` rows each; those of columns that are not there are zeros, which norm gives no weight.
+template <int GT>
+struct RowLogits {
+    float s[GT];
+    __device__ __forceinline__ void load(const float* logits, int64_t stride) {
+#pragma unroll
+        for (int g = 0; g < GT; ++g) s[g] = logits[g * stride];
+    }
+    // sum over the query heads of the row's weights
+    __device__ __forceinline__ float weight(const float2* norm) const {
+        float inc = 0.f;
+#pragma unroll
+        for (int g = 0; g < GT; ++g) inc = fmaf(__builtin_amdgcn_exp2f(s[g] - norm[g].x), norm[g].y, inc);
+        return inc;
+    }
+};
+
+}  // namespace
+
+// GT: bound on the query heads per KV head.
+// Many heads: one workgroup per head does all of the step.  The logits stay in LDS until the sums are known; then every row's weights go to
+// its cum, and the waves' outputs are joined in the same LDS.
+template <typename T, int D, int GT>
+__global__ __launch_bounds__(kAttendThreads, 3) void paged_head_kernel(PagedCache c, const T* __restrict__ q, const T* __restrict__ k_new,
+                                                                    const T* __restrict__ v_new, const int32_t* __restrict__ pos, int G,
+                                                                    int stride, float* __restrict__ out) {
+    using A = WaveAttend<T, D>;
+    extern __shared__ float dyn[];                                        // logits [GT][stride], then outputs [waves][G][D]
+    __shared__ float ml_s[kAttendWaves][16][2];
+    const int h = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, j = lane >> 4;
     const T* kn = k_new + (int64_t)h * D;
     const T* vn = v_new + (int64_t)h * D;
-    float* logits = reinterpret_cast<float*>(ws + p.logit_off) + (int64_t)h * p.rows * G;
-    const float scale2 = kLog2eA * (D == 128 ? 0.08838834764831845f : 0.125f);
-
     A a;
     a.reset();
     a.load_query(col < G ? q + ((int64_t)h * G + col) * D : nullptr, lane);
-    const int in_page = (1 << c.shift) - 1;
-    for (int r0 = begin + A::kBlock * wave; r0 < end; r0 += kStep) {
-        // a block lies in one page, or in two where pages hold sixteen rows
-        const int id0 = table[r0 >> c.shift];
-        const int id1 = A::kBlock > 16 && r0 + 16 < n ? table[(r0 + 16) >> c.shift] : id0;
-        const bool ok0 = page_ok(c, id0), ok1 = page_ok(c, id1);
-        auto row_of = [&](int r) -> int64_t {
-            const int id = r < 16 ? id0 : id1;
-            return ((int64_t)id << c.shift) + ((r0 + r) & in_page);
-        };
-        typename A::Keys keys;
-        typename A::Values values;
-        float s[A::kPerLane];
-        const bool whole = r0 + A::kBlock <= n && ok0 && ok1;
-        if (whole) {
-            A::load_keys(keys, lane, [&](int r) { return K + row_of(r) * D; });
-            A::load_values(values, lane, [&](int r) { return V + row_of(r) * D; });
-            a.logits(keys, scale2, s);
-        } else {
-            // rows behind the last, rows without a page (the pool's first row is read in their place) and the new token
-            auto there = [&](int r) { return r0 + r < n ? (r < 16 ? ok0 : ok1) : joins && r0 + r == n; };
-            A::load_keys(keys, lane, [&](int r) { return !there(r) ? K : r0 + r == n ? kn : K + row_of(r) * D; });
-            A::load_values(values, lane, [&](int r) { return !there(r) ? V : r0 + r == n ? vn : V + row_of(r) * D; });
+    const HeadRows hr = rows_of_head(c, h, k_new != nullptr);
+    const int n1 = hr.n1, blocks = hr.n / A::kBlock;
+    attend_rows<T, D>(a, c, h, hr, kn, vn, A::kBlock * wave, A::kBlock * kAttendWaves, blocks * A::kBlock,
+                      n1 > blocks * A::kBlock && blocks % kAttendWaves == wave, lane, [&](int r, const float (&s)[A::kPerLane]) {
+        if (col < GT)
 #pragma unroll
-            for (int e = 0; e < A::kPerLane; ++e)
-                if (!there(A::value_row(lane, e))) A::clear_value(values, e);
-            a.logits(keys, scale2, s);
-#pragma unroll
-            for (int e = 0; e < A::kPerLane; ++e)
-                if (!there(A::value_row(lane, e))) s[e] = -INFINITY;
-        }
-        if (col < G) {
-#pragma unroll
-            for (int e = 0; e < A::kPerLane; ++e) {
-                const int r = r0 + A::value_row(lane, e);
-                if (r < n1) logits[(int64_t)r * G + col] = s[e];
-            }
-        }
-        take_logits(a, s);
-        a.add_values(values, s);
+            for (int e = 0; e < A::kPerLane; ++e) dyn[col * stride + r + A::value_row(lane, e)] = col < G ? s[e] : 0.f;
+    });
+    const float l = column_sum(a.l);
+    if (j == 0) {
+        ml_s[wave][col][0] = a.m;
+        ml_s[wave][col][1] = l;
     }
+    // four rows a thread at a time, what lies in memory fetched ahead of the sums
+    constexpr int kRows = 4;
+    int64_t at[kRows];
+    float before[kRows];
+    const auto fetch = [&](int r0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int r = r0 + i * kAttendThreads + threadIdx.x;
+            at[i] = r < n1 ? pool_row(c, h, r) : -1;
+            before[i] = at[i] >= 0 && r < hr.n ? c.cum[at[i]] : 0.f;
+        }
+    };
+    fetch(0);
+    __shared__ float2 norm[16];
+    __syncthreads();
+    if (threadIdx.x < 16) {
+        float m = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < kAttendWaves; ++x) m = fmaxf(m, ml_s[x][threadIdx.x][0]);
+        const float ref = reference(m);
+#pragma unroll
+        for (int x = 0; x < kAttendWaves; ++x) sum = fmaf(__builtin_amdgcn_exp2f(ml_s[x][threadIdx.x][0] - ref), ml_s[x][threadIdx.x][1], sum);
+        norm[threadIdx.x] = make_float2(ref, sum == 0.f || (int)threadIdx.x >= G ? 0.f : 1.f / sum);
+    }
+    __syncthreads();
+    for (int r0 = 0; r0 < n1; r0 += kRows * kAttendThreads) {
+        if (r0 > 0) fetch(r0);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int r = r0 + i * kAttendThreads + threadIdx.x;
+            if (at[i] < 0) continue;
+            RowLogits<GT> row;
+            row.load(dyn + r, stride);
+            c.cum[at[i]] = before[i] + row.weight(norm);
+        }
+    }
+    if (hr.joins) write_new_row<T, D>(c, h, hr.n, kn, vn, pos, kAttendThreads);
+    if (out == nullptr) return;
+    __syncthreads();
+    if (col < G) {
+        const float f = __builtin_amdgcn_exp2f(a.m - norm[col].x) * norm[col].y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < A::kVw; t += 4)
+                *reinterpret_cast<f32x4_t*>(dyn + (wave * G + col) * D + A::kVw * (4 * j + i) + t) =
+                    f32x4_t{a.o[t][i] * f, a.o[t + 1][i] * f, a.o[t + 2][i] * f, a.o[t + 3][i] * f};
+    }
+    __syncthreads();
+    for (int e = 4 * threadIdx.x; e < G * D; e += 4 * kAttendThreads) {
+        f32x4_t o = *reinterpret_cast<const f32x4_t*>(dyn + e);
+#pragma unroll
+        for (int x = 1; x < kAttendWaves; ++x) {
+            const f32x4_t v = *reinterpret_cast<const f32x4_t*>(dyn + x * G * D + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] += v[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[(int64_t)h * G * D + e + i] = o[i];
+    }
+}
+
+// Few heads: their rows are dealt to about as many workgroups as run at a time, whatever the heads' lengths: `unit` rows each, the last
+// of a head fewer.  Workgroup number -> head and part, from the lengths, 64 of them at a time.
+struct HeadPart {
+    int h, part, n_parts, unit;
+};
+__device__ __forceinline__ bool find_head_part(const PagedCache& c, int step, const PagedStepPlan& p, int wg, HeadPart* out) {
+    const int lane = threadIdx.x & 63;
+    int64_t total = 0;
+    for (int h = lane; h < c.n_heads; h += 64) total += head_rows(c, h) + 1;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+    const int unit = (int)(((total + p.n_split - 1) / p.n_split + step - 1) / step * step);
+    out->unit = unit;
+    for (int h0 = 0; h0 < c.n_heads; h0 += 64) {
+        const int parts = h0 + lane < c.n_heads ? head_rows(c, h0 + lane) / unit + 1 : 0;      // a head without rows has one too
+        int sum = parts;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += u;
+        }
+        const unsigned long long has = __ballot(sum > wg);
+        if (has != 0) {
+            const int x = __builtin_amdgcn_readfirstlane(__ffsll(has) - 1);
+            out->h = h0 + x;
+            out->n_parts = __builtin_amdgcn_readlane(parts, x);
+            out->part = wg - (__builtin_amdgcn_readlane(sum, x) - out->n_parts);
+            return true;
+        }
+        wg -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
+}
+
+// One part of one head's rows per workgroup, its blocks dealt to the waves in turn.  Leaves the part's maximum, sum and output
+// (joined by the finishing kernel) and every row's logits.
+template <typename T, int D, int GT>
+__global__ __launch_bounds__(kAttendThreads, 3) void paged_attend_kernel(PagedCache c, const T* __restrict__ q, const T* __restrict__ k_new,
+                                                                      const T* __restrict__ v_new, int G, PagedStepPlan p, char* ws) {
+    using A = WaveAttend<T, D>;
+    extern __shared__ float o_s[];                                        // [waves][G][D]
+    __shared__ float ml_s[kAttendWaves][16][2];
+    constexpr int kLine = A::kBlock + 4;
+    __shared__ __align__(16) float line_s[kAttendWaves][GT * kLine];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, j = lane >> 4;
+    constexpr int kStep = A::kBlock * kAttendWaves;
+    HeadPart hp;
+    if (!find_head_part(c, kStep, p, blockIdx.x, &hp)) return;
+    const int h = hp.h;
+    A a;
+    a.reset();
+    a.load_query(col < G ? q + ((int64_t)h * G + col) * D : nullptr, lane);
+    const HeadRows hr = rows_of_head(c, h, k_new != nullptr);
+    const int begin = hp.part * hp.unit, end = begin + hp.unit, blocks = hr.n / A::kBlock;
+    const bool tail = hr.n1 > blocks * A::kBlock && blocks * A::kBlock >= begin && blocks * A::kBlock < end;
+    float* logits = reinterpret_cast<float*>(ws + p.logit_off) + (int64_t)h * GT * p.rows;
+    attend_rows<T, D>(a, c, h, hr, k_new + (int64_t)h * D, v_new + (int64_t)h * D, begin + A::kBlock * wave, kStep, min(end, blocks * A::kBlock),
+                      tail && blocks % kAttendWaves == wave, lane, [&](int r, const float (&s)[A::kPerLane]) {
+        // a wave's logits change places in LDS (in the order its instructions have there) for stores of whole pieces of 16 bytes
+        float* mine = line_s[wave];
+        if (col < GT)
+#pragma unroll
+            for (int e = 0; e < A::kPerLane; ++e) mine[col * kLine + A::value_row(lane, e)] = col < G ? s[e] : 0.f;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int i = 0; i < (GT * A::kBlock + 255) / 256; ++i) {
+            const int x = 4 * (lane + 64 * i), g = x / A::kBlock, in = x % A::kBlock;
+            if (g < GT) *reinterpret_cast<f32x4_t*>(logits + (int64_t)g * p.rows + r + in) = *reinterpret_cast<const f32x4_t*>(mine + g * kLine + in);
+        }
+        __builtin_amdgcn_wave_barrier();
+    });
     // the waves' parts, then the workgroup's
     const float l = column_sum(a.l);
     if (j == 0) {
         ml_s[wave][col][0] = a.m;
         ml_s[wave][col][1] = l;
     }
-#pragma unroll
-    for (int t = 0; t < kVw; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o_s[wave][col][kVw * (4 * j + i) + t] = a.o[t][i];
     __syncthreads();
-    float* acc = reinterpret_cast<float*>(ws + p.acc_off) + ((int64_t)h * n_split + part) * G * D;
-    float* ml = reinterpret_cast<float*>(ws + p.ml_off) + ((int64_t)h * n_split + part) * G * 2;
-    for (int e = threadIdx.x; e < G * D; e += kAttendThreads) {
-        const int g = e / D, d = e % D;
-        float m = ml_s[0][g][0];
+    float m = ml_s[0][col][0];
 #pragma unroll
-        for (int x = 1; x < kAttendWaves; ++x) m = fmaxf(m, ml_s[x][g][0]);
-        const float ref = reference(m);
-        float sum = 0.f, out = 0.f;
+    for (int x = 1; x < kAttendWaves; ++x) m = fmaxf(m, ml_s[x][col][0]);
+    const float ref = reference(m);
+    if (col < G) {
+        const float f = __builtin_amdgcn_exp2f(a.m - ref);
 #pragma unroll
-        for (int x = 0; x < kAttendWaves; ++x) {
-            const float f = __builtin_amdgcn_exp2f(ml_s[x][g][0] - ref);
-            sum = fmaf(f, ml_s[x][g][1], sum);
-            out = fmaf(f, o_s[x][g][d], out);
-        }
-        acc[e] = out;
-        if (d == 0) {
-            ml[2 * g] = m;
-            ml[2 * g + 1] = sum;
-        }
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < A::kVw; t += 4)
+                *reinterpret_cast<f32x4_t*>(o_s + (wave * G + col) * D + A::kVw * (4 * j + i) + t) =
+                    f32x4_t{a.o[t][i] * f, a.o[t + 1][i] * f, a.o[t + 2][i] * f, a.o[t + 3][i] * f};
     }
-    if (part == 0 && threadIdx.x == 0) reinterpret_cast<int2*>(ws + p.head_off)[h] = make_int2(n, n1);
+    if (threadIdx.x < (unsigned)G) {
+        float sum = 0.f;
+#pragma unroll
+        for (int x = 0; x < kAttendWaves; ++x) sum = fmaf(__builtin_amdgcn_exp2f(ml_s[x][col][0] - ref), ml_s[x][col][1], sum);
+        reinterpret_cast<float2*>(ws + p.ml_off)[(int64_t)blockIdx.x * G + col] = make_float2(m, sum);
+    }
+    __syncthreads();
+    float* acc = reinterpret_cast<float*>(ws + p.acc_off) + (int64_t)blockIdx.x * G * D;
+    for (int e = 4 * threadIdx.x; e < G * D; e += 4 * kAttendThreads) {
+        f32x4_t o = *reinterpret_cast<const f32x4_t*>(o_s + e);
+#pragma unroll
+        for (int x = 1; x < kAttendWaves; ++x) o += *reinterpret_cast<const f32x4_t*>(o_s + x * G * D + e);
+        *reinterpret_cast<f32x4_t*>(acc + e) = o;
+    }
+    if (hp.part == 0 && threadIdx.x == 0) reinterpret_cast<int4*>(ws + p.head_off)[h] = make_int4(hr.n, hr.n1, blockIdx.x, hp.n_parts);
 }
 
-// 1024 rows of one head per workgroup: the parts' maxima and sums are joined, every row's weights added to its cum.  The first
-// workgroup of a head also joins the outputs and writes the new row.
-template <typename T, int D>
+// Joins the parts.  The first n_chunks workgroups of a head take 1024 rows each and add their weights to cum; the rest take a share of the
+// outputs, several threads to four features of them; the first also writes the new row.
+template <typename T, int D, int GT>
 __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache c, const T* __restrict__ k_new, const T* __restrict__ v_new,
-                                                                      const int32_t* __restrict__ pos, int G, int n_split, int n_chunks,
+                                                                      const int32_t* __restrict__ pos, int G, int n_chunks, int n_join,
                                                                       PagedStepPlan p, const char* __restrict__ ws, float* __restrict__ out) {
     __shared__ float2 norm[16];
-    const int h = blockIdx.x / n_chunks, chunk = blockIdx.x % n_chunks;
-    const int2 nn = reinterpret_cast<const int2*>(ws + p.head_off)[h];
-    const int n = nn.x, n1 = nn.y;
-    const float* ml = reinterpret_cast<const float*>(ws + p.ml_off) + (int64_t)h * n_split * G * 2;
-    const float* acc = reinterpret_cast<const float*>(ws + p.acc_off) + (int64_t)h * n_split * G * D;
-    if (threadIdx.x < (unsigned)G) {
-        float m = -INFINITY, l = 0.f;
-        for (int s = 0; s < n_split; ++s) {
-            const float ms = ml[(s * G + threadIdx.x) * 2], ls = ml[(s * G + threadIdx.x) * 2 + 1];
-            const float top = fmaxf(m, ms), ref = reference(top);
-            l = l * __builtin_amdgcn_exp2f(m - ref) + ls * __builtin_amdgcn_exp2f(ms - ref);
-            m = top;
+    __shared__ f32x4_t sum_s[kFinishThreads];
+    const int h = blockIdx.x / (n_chunks + n_join), task = blockIdx.x % (n_chunks + n_join);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int4 head = reinterpret_cast<const int4*>(ws + p.head_off)[h];
+    const int n = head.x, n1 = head.y, n_parts = head.w;
+    const float2* ml = reinterpret_cast<const float2*>(ws + p.ml_off) + (int64_t)head.z * G;
+    const bool rows = task < n_chunks;
+    if (rows && task * kFinishRows >= n1 && task > 0) return;
+    // what does not wait for the sums: this thread's rows
+    constexpr int kRows = kFinishRows / kFinishThreads;
+    int64_t at[kRows];
+    float before[kRows];
+    RowLogits<GT> row[kRows];
+    if (rows) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int r = task * kFinishRows + i * kFinishThreads + threadIdx.x;
+            at[i] = r < n1 ? pool_row(c, h, r) : -1;
+            row[i].load(reinterpret_cast<const float*>(ws + p.logit_off) + (int64_t)h * GT * p.rows + min(r, p.rows - 1), p.rows);
         }
-        norm[threadIdx.x] = make_float2(reference(m), l == 0.f ? 0.f : 1.f / l);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) before[i] = at[i] >= 0 && task * kFinishRows + i * kFinishThreads + (int)threadIdx.x < n ? c.cum[at[i]] : 0.f;
+    }
+    // maximum and sum of every query head, a wave each
+    if (threadIdx.x < 16) norm[threadIdx.x] = make_float2(0.f, 0.f);
+    __syncthreads();
+    for (int g = wave; g < G; g += kFinishThreads / 64) {
+        float m = -INFINITY, l = 0.f;
+        for (int s = lane; s < n_parts; s += 64) m = fmaxf(m, ml[s * G + g].x);
+        m = wave_max(m);
+        const float ref = reference(m);
+        for (int s = lane; s < n_parts; s += 64) l = fmaf(__builtin_amdgcn_exp2f(ml[s * G + g].x - ref), ml[s * G + g].y, l);
+        l = wave_sum(l);
+        if (lane == 0) norm[g] = make_float2(ref, l == 0.f ? 0.f : 1.f / l);
     }
     __syncthreads();
-    const float* logits = reinterpret_cast<const float*>(ws + p.logit_off) + (int64_t)h * p.rows * G;
-    for (int r = chunk * kFinishRows + threadIdx.x; r < min(n1, (chunk + 1) * kFinishRows); r += kFinishThreads) {
-        const int64_t at = pool_row(c, h, r);
-        if (at < 0) continue;
-        float w = r < n ? c.cum[at] : 0.f;
-        float inc = 0.f;
-        for (int g = 0; g < G; ++g) inc = fmaf(__builtin_amdgcn_exp2f(logits[(int64_t)r * G + g] - norm[g].x), norm[g].y, inc);
-        c.cum[at] = w + inc;
+    if (rows) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+            if (at[i] >= 0) c.cum[at[i]] = before[i] + row[i].weight(norm);
+        if (task == 0 && n1 > n) write_new_row<T, D>(c, h, n, k_new + (int64_t)h * D, v_new + (int64_t)h * D, pos, kFinishThreads);
+        return;
     }
-    if (chunk != 0) return;
-    if (out != nullptr)
-        for (int e = threadIdx.x; e < G * D; e += kFinishThreads) {
-            const int g = e / D;
-            float o = 0.f;
-            for (int s = 0; s < n_split; ++s) o = fmaf(acc[(int64_t)s * G * D + e], __builtin_amdgcn_exp2f(ml[(s * G + g) * 2] - norm[g].x), o);
-            out[(int64_t)h * G * D + e] = o * norm[g].y;
+    const float* acc = reinterpret_cast<const float*>(ws + p.acc_off) + (int64_t)head.z * G * D;
+    const int quads = (G * D / 4 + n_join - 1) / n_join, groups = kFinishThreads / quads;      // (n_join: quads <= the workgroup's threads)
+    const int quad = (task - n_chunks) * quads + threadIdx.x % quads, group = threadIdx.x / quads;
+    const bool has = group < groups && quad < G * D / 4;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    if (has) {
+        const int g = quad * 4 / D;
+#pragma unroll 4
+        for (int s = group; s < n_parts; s += groups) {
+            const f32x4_t v = *reinterpret_cast<const f32x4_t*>(acc + (int64_t)s * G * D + quad * 4);
+            const float2 w = ml[s * G + g];
+            const float f = __builtin_amdgcn_exp2f(w.x - norm[g].x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = w.y == 0.f ? o[i] : fmaf(f, v[i], o[i]);
         }
-    if (n1 > n) {
-        const int64_t at = pool_row(c, h, n);
-        T* K = static_cast<T*>(c.K);
-        T* V = static_cast<T*>(c.V);
-        for (int d = threadIdx.x; d < D; d += kFinishThreads) {
-            K[at * D + d] = k_new[(int64_t)h * D + d];
-            V[at * D + d] = v_new[(int64_t)h * D + d];
-        }
-        if (threadIdx.x == 0) {
-            c.idx[at] = pos[h];
-            c.len[h] = n1;
-        }
+    }
+    sum_s[threadIdx.x] = o;
+    __syncthreads();
+    if (has && group == 0) {
+        for (int x = 1; x < groups; ++x) o += sum_s[x * quads + threadIdx.x];
+        float* to = out + (int64_t)h * G * D + quad * 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = o[i] * norm[quad * 4 / D].y;
     }
 }
 
@@ -396,23 +646,33 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedCache c, int row_s
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
+namespace {
+int heads_bound(int G) { return G <= 4 ? 4 : G <= 8 ? 8 : 16; }
+// LDS of the one-workgroup step: logits, and later the waves' outputs
+size_t head_step_lds(int G, int D, int rows) {
+    const size_t logits = (size_t)rows * heads_bound(G) * sizeof(float), outputs = (size_t)kAttendWaves * G * D * sizeof(float);
+    return logits > outputs ? logits : outputs;
+}
+}  // namespace
+
 PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows) {
     PagedStepPlan p{};
-    const int blocks = (rows + 127) / 128;
-    int split = (1024 + n_heads - 1) / n_heads;
-    split = split > blocks ? blocks : split;
-    p.n_split = split < 1 ? 1 : (split > 256 ? 256 : split);
-    p.rows = rows;
+    p.rows = (rows + 31) / 32 * 32;                                       // whole blocks are written
+    p.one_launch = n_heads >= kHeadLaunchHeads && head_step_lds(G, D, p.rows) <= kHeadLaunchLds;
+    if (p.one_launch) return p;
+    const int64_t units = (int64_t)n_heads * ((rows + 127) / 128);         // of the fewest rows
+    p.n_split = (int)(units < kSplitAim ? units : kSplitAim);
+    const size_t parts = (size_t)p.n_split + n_heads;                     // every head may end with a broken one
     size_t off = 0;
     auto take = [&](size_t bytes) {
         const size_t at = off;
         off = align_up(off + bytes, 256);
         return at;
     };
-    p.head_off = take((size_t)n_heads * sizeof(int2));
-    p.ml_off = take((size_t)n_heads * p.n_split * G * 2 * sizeof(float));
-    p.acc_off = take((size_t)n_heads * p.n_split * G * D * sizeof(float));
-    p.logit_off = take((size_t)n_heads * rows * G * sizeof(float));
+    p.head_off = take((size_t)n_heads * sizeof(int4));
+    p.ml_off = take(parts * G * sizeof(float2));
+    p.acc_off = take(parts * G * D * sizeof(float));
+    p.logit_off = take((size_t)n_heads * p.rows * heads_bound(G) * sizeof(float));
     p.bytes = off;
     return p;
 }
@@ -443,28 +703,65 @@ hipError_t launch_paged_append(const PagedCache& c, const void* K, const void* V
 }
 
 namespace {
-template <typename T, int D>
+template <typename T, int D, int GT>
 hipError_t step_of(const PagedCache& c, const void* q, const void* k_new, const void* v_new, const int32_t* pos, int G, const PagedStepPlan& p,
                    char* ws, float* out, const Env& env) {
+    const T* kn = static_cast<const T*>(k_new);
+    const T* vn = static_cast<const T*>(v_new);
+    if (p.one_launch) {
+        env.begin("paged_head");
+        paged_head_kernel<T, D, GT><<<c.n_heads, kAttendThreads, head_step_lds(G, D, p.rows), env.s>>>(c, static_cast<const T*>(q), kn, vn, pos, G,
+                                                                                                       p.rows, out);
+        env.end();
+        return hipGetLastError();
+    }
     env.begin("paged_attend");
-    paged_attend_kernel<T, D><<<c.n_heads * p.n_split, kAttendThreads, 0, env.s>>>(
-        c, static_cast<const T*>(q), static_cast<const T*>(k_new), static_cast<const T*>(v_new), G, p.n_split, p, ws);
+    paged_attend_kernel<T, D, GT><<<p.n_split + c.n_heads, kAttendThreads, (size_t)kAttendWaves * G * D * sizeof(float), env.s>>>(
+        c, static_cast<const T*>(q), kn, vn, G, p, ws);
     env.end();
+    // a workgroup joins up to 64 KiB of partial outputs, of at most as many quads as it has threads
     const int n_chunks = (p.rows + kFinishRows - 1) / kFinishRows;
+    const int n_parts = (p.n_split + c.n_heads - 1) / c.n_heads;
+    int n_join = (int)(((int64_t)n_parts * G * D * 4 + 65535) / 65536);
+    const int least = (G * D / 4 + kFinishThreads - 1) / kFinishThreads;
+    n_join = out == nullptr ? 0 : n_join < least ? least : n_join;
     env.begin("paged_finish");
-    paged_finish_kernel<T, D><<<c.n_heads * n_chunks, kFinishThreads, 0, env.s>>>(c, static_cast<const T*>(k_new), static_cast<const T*>(v_new), pos, G,
-                                                                                p.n_split, n_chunks, p, ws, out);
+    paged_finish_kernel<T, D, GT><<<c.n_heads * (n_chunks + n_join), kFinishThreads, 0, env.s>>>(c, kn, vn, pos, G, n_chunks, n_join, p, ws, out);
     env.end();
     return hipGetLastError();
 }
+
+// calls f with the kernels' types: element, head width, bound on the query heads
+template <typename F>
+hipError_t with_types(uncomp_dtype dt, int D, int G, F&& f) {
+    const auto bound = [&](auto t, auto d) {
+        if (G <= 4) return f(t, d, std::integral_constant<int, 4>{});
+        if (G <= 8) return f(t, d, std::integral_constant<int, 8>{});
+        return f(t, d, std::integral_constant<int, 16>{});
+    };
+    const auto width = [&](auto t) { return D == 128 ? bound(t, std::integral_constant<int, 128>{}) : bound(t, std::integral_constant<int, 64>{}); };
+    return dt == UNCOMP_BF16 ? width(bf16_bits{}) : width(float{});
+}
 }  // namespace
+
+hipError_t init_paged_kernels() {
+    for (uncomp_dtype dt : {UNCOMP_BF16, UNCOMP_F32})
+        for (int D : {64, 128})
+            for (int G : {4, 8, 16}) {
+                const hipError_t e = with_types(dt, D, G, [](auto t, auto d, auto g) {
+                    return allow_dynamic_lds(reinterpret_cast<const void*>(paged_head_kernel<decltype(t), decltype(d)::value, decltype(g)::value>),
+                                             kHeadLaunchLds);
+                });
+                if (e != hipSuccess) return e;
+            }
+    return hipSuccess;
+}
 
 hipError_t launch_paged_step(const PagedCache& c, const void* q, const void* k_new, const void* v_new, uncomp_dtype dt, const int32_t* pos, int G,
                              int D, const PagedStepPlan& p, char* ws, float* out, const Env& env) {
-    if (dt == UNCOMP_BF16)
-        return D == 128 ? step_of<bf16_bits, 128>(c, q, k_new, v_new, pos, G, p, ws, out, env)
-                        : step_of<bf16_bits, 64>(c, q, k_new, v_new, pos, G, p, ws, out, env);
-    return D == 128 ? step_of<float, 128>(c, q, k_new, v_new, pos, G, p, ws, out, env) : step_of<float, 64>(c, q, k_new, v_new, pos, G, p, ws, out, env);
+    return with_types(dt, D, G, [&](auto t, auto d, auto g) {
+        return step_of<decltype(t), decltype(d)::value, decltype(g)::value>(c, q, k_new, v_new, pos, G, p, ws, out, env);
+    });
 }
 
 hipError_t launch_paged_evict(const PagedCache& c, const int32_t* budget, const int32_t* pos, int w, int row_size, const PagedEvictPlan& p, char* ws,

@@ -204,10 +204,11 @@ __global__ __launch_bounds__(256) void prefill_f32_kernel(PrefillArgs a) {
     at.load_query(Q, lane);
     typename A::Keys keys;
     typename A::Values values;
-    const auto fetch_keys = [&](int r0) { A::load_keys(keys, lane, [&](int r) { return K + min(r0 + r, w.keys - 1) * a.k.sr; }); };
+    const auto fetch_keys = [&](int r0) { A::load_key(keys, lane, K + min(r0 + A::key_row(lane, 0), w.keys - 1) * a.k.sr); };
     if (end > 0) fetch_keys(0);
     for (int r0 = 0; r0 < end; r0 += A::kBlock) {
-        A::load_values(values, lane, [&](int r) { return V + min(r0 + r, w.keys - 1) * a.v.sr; });
+#pragma unroll
+        for (int e = 0; e < A::kPerLane; ++e) A::load_value(values, lane, e, V + min(r0 + A::value_row(lane, e), w.keys - 1) * a.v.sr);
         float p[A::kPerLane];
         at.logits(keys, scale2, p);
         fetch_keys(r0 + A::kBlock);
