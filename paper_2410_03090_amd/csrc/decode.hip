@@ -743,14 +743,6 @@ __global__ __launch_bounds__(NT) void decode_update_kernel(
 // 5120 heads of 768 rows on average, 8 query heads: 453 + 69 us in two kernels, 405 here; 256 heads of 2048 rows: 58 + 12, 55.
 constexpr float kRefSlack = 40.f;
 
-// Head of workgroup b.  Workgroups go to the eight XCDs in turn, and lengths often repeat with the head's number (the
-// budgets of a layer's eight heads): in order, one XCD would get all the long ones.  Every eight heads are turned by
-// another amount instead (1000 heads of 1450 rows, every sixteenth full and the others an eighth: 65 -> 42 us).
-__device__ __forceinline__ int spread_head(unsigned b, unsigned n) {
-    const unsigned o = b >> 3;
-    return b < (n & ~7u) ? 8 * o + ((b + o + (o >> 1) + (o >> 2) + (o >> 3)) & 7) : b;
-}
-
 template <int GT, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void decode_head_kernel(
     const bf16_bits* __restrict__ q, const bf16_bits* __restrict__ k_new, const bf16_bits* __restrict__ v_new, int G,

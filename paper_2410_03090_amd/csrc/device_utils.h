@@ -95,4 +95,12 @@ __device__ __forceinline__ void each16(F&& f) {
     }
 }
 
+// Head of workgroup b.  Workgroups go to the eight XCDs in turn, and lengths often repeat with the head's number (the
+// budgets of a layer's eight heads): in order, one XCD would get all the long ones.  Every eight heads are turned by
+// another amount instead (1000 heads of 1450 rows, every sixteenth full and the others an eighth: 65 -> 42 us).
+__device__ __forceinline__ int spread_head(unsigned b, unsigned n) {
+    const unsigned o = b >> 3;
+    return b < (n & ~7u) ? 8 * o + ((b + o + (o >> 1) + (o >> 2) + (o >> 3)) & 7) : b;
+}
+
 }  // namespace uncomp

@@ -167,6 +167,7 @@ __device__ __forceinline__ void attend_rows(WaveAttend<T, D>& a, const PagedCach
     if (first >= end) return;
     Pages p = pages_of(first), next = pages_of(first + step);
     load_keys(p, first);
+    __builtin_amdgcn_sched_barrier(0);                                    // in this order: the wait for the keys leaves the values on their way
     load_values(p, first);
     for (int r0 = first; r0 < end; r0 += step) {
         float s[A::kPerLane];
@@ -200,6 +201,29 @@ __device__ __forceinline__ void write_new_row(const PagedCache& c, int h, int n,
     }
 }
 
+// Where N rows of head h, `step` apart, are in the pool (-1: not there), and their cumulative scores, that of row n being zero.  All loads are
+// made, from row 0 of the pool where there is none, so that they do not wait for one another.
+template <int N>
+struct RowPlaces {
+    int64_t at[N];
+    float cum[N];
+    __device__ __forceinline__ void fetch(const PagedCache& c, int h, int first, int step, int n, int n1) {
+        int id[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) id[i] = c.table[(int64_t)h * c.max_pages + min((first + i * step) >> c.shift, c.max_pages - 1)];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int r = first + i * step;
+            const bool has = r < n1 && page_ok(c, id[i]);
+            at[i] = ((int64_t)(has ? id[i] : 0) << c.shift) + (has ? r & ((1 << c.shift) - 1) : 0);
+            cum[i] = c.cum[at[i]];
+            if (!has) at[i] = -1;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) cum[i] = first + i * step < n ? cum[i] : 0.f;
+    }
+};
+
 // Logits lie query head by query head, `stride` rows each; those of columns that are not there are zeros, which norm gives no weight.
 template <int GT>
 struct RowLogits {
@@ -229,7 +253,7 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_head_kernel(PagedCach
     using A = WaveAttend<T, D>;
     extern __shared__ float dyn[];                                        // logits [GT][stride], then outputs [waves][G][D]
     __shared__ float ml_s[kAttendWaves][16][2];
-    const int h = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, j = lane >> 4;
+    const int h = spread_head(blockIdx.x, gridDim.x), lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, j = lane >> 4;
     const T* kn = k_new + (int64_t)h * D;
     const T* vn = v_new + (int64_t)h * D;
     A a;
@@ -250,17 +274,8 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_head_kernel(PagedCach
     }
     // four rows a thread at a time, what lies in memory fetched ahead of the sums
     constexpr int kRows = 4;
-    int64_t at[kRows];
-    float before[kRows];
-    const auto fetch = [&](int r0) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int r = r0 + i * kAttendThreads + threadIdx.x;
-            at[i] = r < n1 ? pool_row(c, h, r) : -1;
-            before[i] = at[i] >= 0 && r < hr.n ? c.cum[at[i]] : 0.f;
-        }
-    };
-    fetch(0);
+    RowPlaces<kRows> places;
+    places.fetch(c, h, threadIdx.x, kAttendThreads, hr.n, n1);
     __shared__ float2 norm[16];
     __syncthreads();
     if (threadIdx.x < 16) {
@@ -273,16 +288,14 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_head_kernel(PagedCach
         norm[threadIdx.x] = make_float2(ref, sum == 0.f || (int)threadIdx.x >= G ? 0.f : 1.f / sum);
     }
     __syncthreads();
-    for (int r0 = 0; r0 < n1; r0 += kRows * kAttendThreads) {
-        if (r0 > 0) fetch(r0);
+    for (int r0 = threadIdx.x; r0 < n1; r0 += kRows * kAttendThreads) {
+        if (r0 >= kRows * kAttendThreads) places.fetch(c, h, r0, kAttendThreads, hr.n, n1);
+        RowLogits<GT> row[kRows];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int r = r0 + i * kAttendThreads + threadIdx.x;
-            if (at[i] < 0) continue;
-            RowLogits<GT> row;
-            row.load(dyn + r, stride);
-            c.cum[at[i]] = before[i] + row.weight(norm);
-        }
+        for (int i = 0; i < kRows; ++i) row[i].load(dyn + min(r0 + i * kAttendThreads, stride - 1), stride);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+            if (places.at[i] >= 0) c.cum[places.at[i]] = places.cum[i] + row[i].weight(norm);
     }
     if (hr.joins) write_new_row<T, D>(c, h, hr.n, kn, vn, pos, kAttendThreads);
     if (out == nullptr) return;
@@ -437,18 +450,14 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache
     if (rows && task * kFinishRows >= n1 && task > 0) return;
     // what does not wait for the sums: this thread's rows
     constexpr int kRows = kFinishRows / kFinishThreads;
-    int64_t at[kRows];
-    float before[kRows];
+    RowPlaces<kRows> places;
     RowLogits<GT> row[kRows];
     if (rows) {
+        const int first = task * kFinishRows + threadIdx.x;
+        const float* logits = reinterpret_cast<const float*>(ws + p.logit_off) + (int64_t)h * GT * p.rows;
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int r = task * kFinishRows + i * kFinishThreads + threadIdx.x;
-            at[i] = r < n1 ? pool_row(c, h, r) : -1;
-            row[i].load(reinterpret_cast<const float*>(ws + p.logit_off) + (int64_t)h * GT * p.rows + min(r, p.rows - 1), p.rows);
-        }
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) before[i] = at[i] >= 0 && task * kFinishRows + i * kFinishThreads + (int)threadIdx.x < n ? c.cum[at[i]] : 0.f;
+        for (int i = 0; i < kRows; ++i) row[i].load(logits + min(first + i * kFinishThreads, p.rows - 1), p.rows);
+        places.fetch(c, h, first, kFinishThreads, n, n1);
     }
     // maximum and sum of every query head, a wave each
     if (threadIdx.x < 16) norm[threadIdx.x] = make_float2(0.f, 0.f);
@@ -466,7 +475,7 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache
     if (rows) {
 #pragma unroll
         for (int i = 0; i < kRows; ++i)
-            if (at[i] >= 0) c.cum[at[i]] = before[i] + row[i].weight(norm);
+            if (places.at[i] >= 0) c.cum[places.at[i]] = places.cum[i] + row[i].weight(norm);
         if (task == 0 && n1 > n) write_new_row<T, D>(c, h, n, k_new + (int64_t)h * D, v_new + (int64_t)h * D, pos, kFinishThreads);
         return;
     }
@@ -661,7 +670,9 @@ PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows) {
     p.one_launch = n_heads >= kHeadLaunchHeads && head_step_lds(G, D, p.rows) <= kHeadLaunchLds;
     if (p.one_launch) return p;
     const int64_t units = (int64_t)n_heads * ((rows + 127) / 128);         // of the fewest rows
-    p.n_split = (int)(units < kSplitAim ? units : kSplitAim);
+    // broken parts count half: together about as many as run at a time; of more heads than that, several rounds
+    const int aim = n_heads < kHeadLaunchHeads ? kSplitAim - n_heads / 2 : 4 * kSplitAim;
+    p.n_split = (int)(units < aim ? units : aim);
     const size_t parts = (size_t)p.n_split + n_heads;                     // every head may end with a broken one
     size_t off = 0;
     auto take = [&](size_t bytes) {
