@@ -437,7 +437,7 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
  * what it points to is DEVICE memory owned by the caller.  The caller hands pages out: a page
  * belongs to one head and stands in its table once.  A table entry outside [0, n_pages) is no page;
  * rows there are not attended to and not written.  page is 16, 32, 64, 128 or 256;
- * max_pages*page <= 2^26; D 64 or 128; K_pages and V_pages 16-byte aligned.
+ * max_pages*page <= 2^26; n_pages*page < 2^31; D 64 or 128; K_pages and V_pages 16-byte aligned.
  * Workspace of the three calls: uncomp_paged_workspace_bytes, rows = max_pages*page.
  */
 typedef struct {
@@ -485,7 +485,8 @@ uncomp_status uncomp_paged_step(uncomp_ctx* ctx, const uncomp_paged_cache* cache
  * lower position, equal positions by lower row; a NaN score counts as more than any number.  The rows
  * behind the new end that stay then move, in order, into the gaps before it, so that the pages behind
  * it hold nothing; len[h] becomes the new end.  evicted [n_heads] (may be NULL) gets the number of rows
- * that left.  The contents of rows behind the new end are unspecified.  w >= 0.
+ * that left.  The contents of rows behind the new end are unspecified.  A head whose table lacks a page
+ * for one of its rows is left as it is.  w >= 0.
  */
 uncomp_status uncomp_paged_evict(uncomp_ctx* ctx, const uncomp_paged_cache* cache, const int32_t* budget,
                                  const int32_t* pos, int w, int32_t* evicted, void* stream);

@@ -10,7 +10,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import NamedTuple
 
 import torch
 
@@ -37,19 +36,35 @@ EXPORTS = (
 _lib = None
 
 
-class PagedCache(NamedTuple):
-    """Rows of every KV head in pages of one pool; the tensors are updated in place by the paged calls."""
-    K: torch.Tensor          # [n_pages, page, D]
-    V: torch.Tensor          # [n_pages, page, D]
-    idx: torch.Tensor        # [n_pages, page] int32: original positions
-    cum: torch.Tensor        # [n_pages, page] float32: cumulative scores
-    table: torch.Tensor      # [n_heads, max_pages] int32: page numbers, anything outside the pool for no page
-    length: torch.Tensor     # [n_heads] int32: rows in use
-
-
 class _PagedCacheStruct(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("K_pages", "V_pages", "idx_pages", "cum_pages", "table", "len")] + \
                [(n, ctypes.c_int) for n in ("dtype", "n_heads", "n_pages", "page", "max_pages", "D")]
+
+
+class PagedCache:
+    """Rows of every KV head in pages of one pool.  The tensors are updated in place by the paged calls and may be written to by the
+    caller; checked once, here, they stay where they are for the life of the object.
+
+    K, V [n_pages, page, D]; idx [n_pages, page] int32: original positions; cum [n_pages, page] float32: cumulative scores;
+    table [n_heads, max_pages] int32: page numbers, anything outside the pool for no page; length [n_heads] int32: rows in use."""
+
+    __slots__ = ("K", "V", "idx", "cum", "table", "length", "n_heads", "D", "dtype", "device", "_struct", "_ref")
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, idx: torch.Tensor, cum: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
+        n_pages, page, D = K.shape
+        n_heads, max_pages = table.shape
+        assert V.shape == K.shape and V.dtype == K.dtype and idx.shape == cum.shape == (n_pages, page)
+        assert idx.dtype == table.dtype == length.dtype == torch.int32 and cum.dtype == torch.float32 and length.shape == (n_heads,)
+        for t in (K, V, idx, cum, table, length):
+            assert t.is_contiguous() and t.is_cuda and t.device == K.device
+        self.K, self.V, self.idx, self.cum, self.table, self.length = K, V, idx, cum, table, length
+        self.n_heads, self.D, self.dtype, self.device = n_heads, D, K.dtype, K.device
+        self._struct = _PagedCacheStruct(K.data_ptr(), V.data_ptr(), idx.data_ptr(), cum.data_ptr(), table.data_ptr(), length.data_ptr(),
+                                         _dtype_code(K), n_heads, n_pages, page, max_pages, D)
+        self._ref = ctypes.byref(self._struct)
+
+    def __iter__(self):
+        return iter((self.K, self.V, self.idx, self.cum, self.table, self.length))
 
 
 class UncompError(RuntimeError):
@@ -155,8 +170,17 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError(f"unsupported dtype {t.dtype}")
 
 
-def _stream(device=None) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+def _stream() -> int:
+    return torch.cuda.current_stream().cuda_stream
+
+
+_I64x2, _I64x3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
+
+
+def _strides(t: torch.Tensor):
+    """(sequence, head, row) strides of [..., heads, rows, D]; a dimension of one entry has any stride, [heads, rows, D] no sequences."""
+    n, s = t.shape, t.stride()
+    return _I64x3(s[0] if len(n) == 4 and n[0] > 1 else 0, s[-3] if n[-3] > 1 else 0, s[-2] if n[-2] > 1 else n[-1])
 
 
 def _ptr(t):
@@ -229,6 +253,10 @@ class Context:
     def _check(self, st: int):
         if st != OK:
             raise UncompError(st, self.lib.uncomp_last_error(self.handle).decode())
+
+    def _raw_stream(self) -> int:
+        """torch's current stream of the context's device, whichever device is current (without the Stream object, which takes 2 us)."""
+        return torch._C._cuda_getCurrentRawStream(self.device)
 
     def profile(self, on: bool):
         self._check(self.lib.uncomp_profile(self.handle, 1 if on else 0))
@@ -463,41 +491,28 @@ class Context:
         rows of every sequence, where not all or not up to the next start.  The index tensors are int32 on the device.
         Returns out (shape and dtype of Q) and lse, float32 [B, H*G, Nq] or [H*G, T] (None without want_lse); fresh
         outputs are zeros (lse -inf) where no sequence has a row."""
-        def rows(t, first):
-            assert t.dim() == (3 if first is not None else 4) and t.stride(-1) == 1
-            return t.unsqueeze(0) if first is not None else t
-
-        def strides(t):
-            # a dimension of one entry has any stride
-            s = [d if n == 1 else st for d, n, st in zip((0, 0, t.shape[3]), t.shape, t.stride())]
-            return (ctypes.c_int64 * 3)(*s)
-
-        Q4, K4, V4 = rows(Q, q_first), rows(K, k_first), rows(V, k_first)
-        Hq, Nq, D = Q4.shape[1:]
-        H, Nk = K4.shape[1], K4.shape[2]
+        assert Q.dim() == (4 if q_first is None else 3) and K.dim() == (4 if k_first is None else 3) and K.shape == V.shape
+        Hq, Nq, D = Q.shape[-3:]
+        H, Nk, Dk = K.shape[-3:]
+        n_seq = Q.shape[0] if q_first is None else q_first.numel() - (q_len is None)
+        assert n_seq == (K.shape[0] if k_first is None else k_first.numel() - (k_len is None)), "as many sequences of keys as of queries"
         for t in (q_first, k_first, q_len, k_len):
             assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.device == Q.device)
-        counts = {x for x in (None if q_first is None else q_first.numel() - (q_len is None), None if q_len is None else q_len.numel(),
-                              None if k_first is None else k_first.numel() - (k_len is None), None if k_len is None else k_len.numel(),
-                              None if q_first is not None else Q4.shape[0], None if k_first is not None else K4.shape[0]) if x is not None}
-        assert len(counts) == 1, "sequences are counted differently by the arguments"
-        n_seq = counts.pop()
-        assert Hq == H * G and K.shape == V.shape and K4.shape[3] == D and Q.dtype == K.dtype == V.dtype
+        assert (q_len is None or q_len.numel() == n_seq) and (k_len is None or k_len.numel() == n_seq)
+        assert Hq == H * G and Dk == D and Q.dtype == K.dtype == V.dtype and Q.stride(-1) == K.stride(-1) == V.stride(-1) == 1
         assert Q.device == K.device == V.device and Q.device.index == self.device
         if out is None:
             out = torch.zeros_like(Q)
-        assert out.shape == Q.shape and out.dtype == Q.dtype and out.device == Q.device
+        assert out.shape == Q.shape and out.dtype == Q.dtype and out.device == Q.device and out.stride(-1) == 1
         if lse is None and want_lse:
             lse = torch.full(Q.shape[:-1], float("-inf"), dtype=torch.float32, device=Q.device)
         ls = None
         if lse is not None:
             assert lse.shape == Q.shape[:-1] and lse.dtype == torch.float32 and lse.stride(-1) == 1 and lse.device == Q.device
-            ls = (ctypes.c_int64 * 2)(*((0, lse.stride(0)) if q_first is not None else lse.stride()[:2]))
-        O4 = rows(out, q_first)
+            ls = _I64x2(lse.stride(0) if q_first is None else 0, lse.stride(-2))
         self._check(self.lib.uncomp_prefill_attention(
             self.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), _dtype_code(Q), n_seq, H, int(G), D, Nq, Nk, _ptr(q_first), _ptr(q_len),
-            _ptr(k_first), _ptr(k_len), strides(Q4), strides(K4), strides(V4), out.data_ptr(),
-            strides(O4), _ptr(lse), ls, _stream(Q.device)))
+            _ptr(k_first), _ptr(k_len), _strides(Q), _strides(K), _strides(V), out.data_ptr(), _strides(out), _ptr(lse), ls, self._raw_stream()))
         return out, lse
 
     # -- paged cache -----------------------------------------------------------------------------
@@ -509,47 +524,40 @@ class Context:
                           table=torch.full((n_heads, max_pages), -1, dtype=torch.int32, **kw),
                           length=torch.zeros(n_heads, dtype=torch.int32, **kw))
 
-    def _paged(self, c: PagedCache):
-        n_pages, page, D = c.K.shape
-        n_heads, max_pages = c.table.shape
-        assert c.V.shape == c.K.shape and c.V.dtype == c.K.dtype and c.idx.shape == c.cum.shape == (n_pages, page)
-        assert c.idx.dtype == c.table.dtype == c.length.dtype == torch.int32 and c.cum.dtype == torch.float32
-        assert c.length.shape == (n_heads,)
-        for t in c:
-            assert t.is_contiguous() and t.device.index == self.device
-        return ctypes.byref(_PagedCacheStruct(c.K.data_ptr(), c.V.data_ptr(), c.idx.data_ptr(), c.cum.data_ptr(), c.table.data_ptr(),
-                                              c.length.data_ptr(), _dtype_code(c.K), n_heads, n_pages, page, max_pages, D))
-
     def paged_append(self, cache: PagedCache, K: torch.Tensor, V: torch.Tensor, idx: torch.Tensor, cum=None, rows=None):
         """K / V [n_heads, cap, D] (last dim contiguous), idx [n_heads, cap] int32, cum [n_heads, cap] float32 or None (zeros), rows
         [n_heads] int32 the rows offered of every head (None: all).  cache.length tells what was taken."""
         n_heads, cap, D = K.shape
-        assert K.shape == V.shape and K.stride() == V.stride() and K.stride(2) == 1 and K.dtype == V.dtype == cache.K.dtype
-        assert n_heads == cache.length.numel() and D == cache.K.shape[2]
+        assert K.shape == V.shape and K.stride() == V.stride() and K.stride(2) == 1 and K.dtype == V.dtype == cache.dtype
+        assert n_heads == cache.n_heads and D == cache.D and cache.device.index == self.device
         assert idx.shape == (n_heads, cap) and idx.dtype == torch.int32 and idx.is_contiguous()
         assert cum is None or (cum.shape == (n_heads, cap) and cum.dtype == torch.float32 and cum.is_contiguous())
         assert rows is None or (rows.shape == (n_heads,) and rows.dtype == torch.int32 and rows.is_contiguous())
         for t in (K, V, idx, cum, rows):
-            assert t is None or t.device == cache.K.device
-        strides = (ctypes.c_int64 * 2)(0 if n_heads == 1 else K.stride(0), D if cap == 1 else K.stride(1))
-        self._check(self.lib.uncomp_paged_append(self.handle, self._paged(cache), K.data_ptr(), V.data_ptr(), idx.data_ptr(), _ptr(cum),
-                                                 _ptr(rows), cap, strides, _stream(K.device)))
+            assert t is None or t.device == cache.device
+        strides = _I64x2(K.stride(0) if n_heads > 1 else 0, K.stride(1) if cap > 1 else D)
+        self._check(self.lib.uncomp_paged_append(self.handle, cache._ref, K.data_ptr(), V.data_ptr(), idx.data_ptr(), _ptr(cum), _ptr(rows), cap,
+                                                 strides, self._raw_stream()))
 
     def paged_step(self, cache: PagedCache, q: torch.Tensor, k_new=None, v_new=None, pos=None, out=None, want_out: bool = True):
         """q [n_heads, G, D], k_new / v_new [n_heads, D], pos [n_heads] int32 (the three may be None together).  Returns out
         [n_heads, G, D] float32; the cache is updated in place."""
-        n_heads, G, D = q.shape
-        assert n_heads == cache.length.numel() and D == cache.K.shape[2] and q.dtype == cache.K.dtype and q.is_contiguous()
+        shape, device = q.shape, cache.device
+        n_heads, G, D = shape
+        assert n_heads == cache.n_heads and D == cache.D and q.dtype == cache.dtype and q.is_contiguous() and q.device == device
+        assert device.index == self.device
         if k_new is not None:
-            assert k_new.shape == v_new.shape == (n_heads, D) and k_new.dtype == v_new.dtype == cache.K.dtype
+            assert k_new.shape == v_new.shape == (n_heads, D) and k_new.dtype == v_new.dtype == cache.dtype
             assert pos.shape == (n_heads,) and pos.dtype == torch.int32
+            assert k_new.is_contiguous() and v_new.is_contiguous() and pos.is_contiguous()
+            assert k_new.device == v_new.device == pos.device == device
+        else:
+            assert v_new is None and pos is None
         if out is None and want_out:
-            out = torch.empty(n_heads, G, D, dtype=torch.float32, device=q.device)
-        assert out is None or (out.shape == q.shape and out.dtype == torch.float32)
-        for t in (q, k_new, v_new, pos, out):
-            assert t is None or (t.is_contiguous() and t.device == cache.K.device)
-        self._check(self.lib.uncomp_paged_step(self.handle, self._paged(cache), q.data_ptr(), G, _ptr(k_new), _ptr(v_new), _ptr(pos),
-                                               _ptr(out), _stream(q.device)))
+            out = torch.empty(shape, dtype=torch.float32, device=device)
+        assert out is None or (out.shape == shape and out.dtype == torch.float32 and out.is_contiguous() and out.device == device)
+        self._check(self.lib.uncomp_paged_step(self.handle, cache._ref, q.data_ptr(), G, _ptr(k_new), _ptr(v_new), _ptr(pos), _ptr(out),
+                                               self._raw_stream()))
         return out
 
     def paged_evict(self, cache: PagedCache, budget: torch.Tensor, pos: torch.Tensor, w: int, evicted=None):
@@ -558,7 +566,8 @@ class Context:
         if evicted is None:
             evicted = torch.empty_like(cache.length)
         for t in (budget, pos, evicted):
-            assert t.shape == cache.length.shape and t.dtype == torch.int32 and t.is_contiguous() and t.device == cache.K.device
-        self._check(self.lib.uncomp_paged_evict(self.handle, self._paged(cache), budget.data_ptr(), pos.data_ptr(), int(w),
-                                                evicted.data_ptr(), _stream(budget.device)))
+            assert t.shape == (cache.n_heads,) and t.dtype == torch.int32 and t.is_contiguous() and t.device == cache.device
+        assert cache.device.index == self.device
+        self._check(self.lib.uncomp_paged_evict(self.handle, cache._ref, budget.data_ptr(), pos.data_ptr(), int(w), evicted.data_ptr(),
+                                                self._raw_stream()))
         return evicted

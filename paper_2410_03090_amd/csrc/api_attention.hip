@@ -58,6 +58,7 @@ uncomp_status check_paged(uncomp_ctx* ctx, const char* who, const uncomp_paged_c
     while (shift < 8 && (1 << shift) != c->page) ++shift;
     if ((1 << shift) != c->page) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: pages hold 16, 32, 64, 128 or 256 rows", who);
     if ((int64_t)c->max_pages * c->page > 1 << 26) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: more than 2^26 rows per head", who);
+    if ((int64_t)c->n_pages * c->page > 0x7fffffffLL) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 rows in the pool", who);
     if ((int64_t)c->n_heads * 256 > 0x7fffffffLL) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: too many heads", who);
     if (!aligned16(c->K_pages) || !aligned16(c->V_pages)) return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: 16-byte aligned pages required", who);
     if (!aligned4(c->idx_pages) || !aligned4(c->cum_pages) || !aligned4(c->table) || !aligned4(c->len))

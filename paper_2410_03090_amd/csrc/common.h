@@ -284,7 +284,8 @@ PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows);
 struct PagedEvictPlan {
     int pairs;           // most rows of one head that move
     size_t count_off;    // int32 [n_heads]
-    size_t pair_off;     // int2  [n_heads][pairs]: to, from
+    size_t pair_off;     // int2  [n_heads][pairs]: to, from (rows of the pool)
+    int n_keys;          // keys of a head that the selection holds in LDS
     size_t bytes;
 };
 PagedEvictPlan plan_paged_evict(int n_heads, int rows);

@@ -17,7 +17,7 @@ constexpr int kSplitAim = 768;                        // workgroups of the atten
 // One workgroup a head: from as many heads on as fill the chip, with logits that leave room for two workgroups on a CU.
 constexpr int kHeadLaunchHeads = 512;
 constexpr size_t kHeadLaunchLds = 76 * 1024;
-constexpr int kSelectThreads = 1024;
+constexpr int kSelectThreads = 1024, kSelectKeys = 32768;         // threads of a selection, keys that it holds in LDS
 
 __device__ __forceinline__ int head_rows(const PagedCache& c, int h) {
     const int cap = c.max_pages << c.shift;
@@ -506,23 +506,22 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache
 }
 
 // ---- eviction --------------------------------------------------------------------------------------------------------
+// Rows leave in the order of (accumulated weight, position, row).  A row's key is its weight as an unsigned number of the same
+// order; the key of the last one to leave is searched for, and only where equal keys lie on both sides of the cut the same is
+// done with their positions, and with equal positions in row order.  The i-th gap before the new end is then paired with the i-th survivor
+// behind it, as rows of the pool, and another kernel moves the rows.
 namespace {
-// Rows leave in the order of (accumulated weight, position, row).  A NaN counts as more than any number.
-__device__ __forceinline__ uint32_t weight_key(float f) { return f != f ? 0xffffffffu : order_key(f); }
+constexpr uint32_t kStays = 0xffffffffu;                // the key of a row that may not leave: above every other
+
+__device__ __forceinline__ uint32_t weight_key(float f) { return f != f ? kStays - 1 : order_key(f); }
 __device__ __forceinline__ uint32_t position_key(int32_t p) { return (uint32_t)p ^ 0x80000000u; }
 
-__device__ __forceinline__ int block_sum(int v, int* buf) {
-    const int wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) buf[wave] = v;
-    __syncthreads();
-    int t = 0;
-#pragma unroll
-    for (int i = 0; i < kSelectThreads / 64; ++i) t += buf[i];
-    return t;
+// how many rows a head has to give up, were they all old enough
+__device__ __forceinline__ int rows_over(int n, int budget, int w) {
+    const int b = max(budget, w);
+    return n > b ? n - b : 0;
 }
+
 // sum of v over the threads before this one, and over all
 __device__ __forceinline__ int block_scan(int v, int* buf, int* total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -544,96 +543,259 @@ __device__ __forceinline__ int block_scan(int v, int* buf, int* total) {
     *total = t;
     return before + s - v;
 }
+
+// The `want` smallest of the keys that each(f) hands to f, by a histogram of 1024 bins over what is left of their range, ten bits a
+// round (the workgroup's threads together; at least `want` keys).  Returns the key of the last of them; *left: how many
+// keys equal to it are among them (INT_MAX: all).
+template <typename F>
+__device__ uint32_t last_of_smallest(F&& each, int want, int* hist, int* buf, uint32_t* range, int* pick, int* left) {
+    const int tid = threadIdx.x;
+    uint32_t lo = 0xffffffffu, hi = 0u;
+    each([&](uint32_t k) {
+        lo = min(lo, k);
+        hi = max(hi, k);
+    });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+    }
+    if (tid == 0) {
+        range[0] = 0xffffffffu;
+        range[1] = 0u;
+    }
+    __syncthreads();
+    if ((tid & 63) == 0) {
+        atomicMin(&range[0], lo);
+        atomicMax(&range[1], hi);
+    }
+    __syncthreads();
+    lo = range[0];
+    hi = range[1];
+    while (true) {
+        const int bits = hi == lo ? 0 : 32 - __clz((int)(hi - lo)), shift = bits > 10 ? bits - 10 : 0;
+        hist[tid] = 0;
+        __syncthreads();
+        each([&](uint32_t k) {
+            if (k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1);
+        });
+        __syncthreads();
+        int total;
+        const int here = hist[tid], before = block_scan(here, buf, &total);
+        if (before < want && before + here >= want) {
+            pick[0] = tid;
+            pick[1] = before;
+            pick[2] = here;
+        }
+        __syncthreads();
+        want -= pick[1];
+        lo += (uint32_t)pick[0] << shift;
+        if (hi - lo >= 1u << shift) hi = lo + ((1u << shift) - 1u);
+        const bool all = pick[2] == want;
+        __syncthreads();
+        if (all || shift == 0) {
+            *left = all ? 0x7fffffff : want;
+            return hi;
+        }
+    }
+}
 }  // namespace
 
-// One workgroup per head finds the rows that leave (radix selection over the 64 bits of weight and position, eight at a time, then
-// the row among equals) and pairs the i-th gap before the new end with the i-th survivor behind it.
-__global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos,
-                                                                      int w, PagedEvictPlan p, char* ws, int32_t* __restrict__ evicted) {
-    __shared__ int hist[256];
-    __shared__ int buf[kSelectThreads / 64];
-    __shared__ int pick[2];
-    const int h = blockIdx.x, tid = threadIdx.x;
-    const int n = head_rows(c, h);
+// Short tables (at most 64 R rows): a wave per head, every row's key in a register, the cut found bit by bit with a count of the
+// keys below it; no workgroup has to wait for anything.
+template <int R>
+__global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos,
+                                                                int w, PagedEvictPlan p, char* ws, int32_t* __restrict__ evicted) {
+    const int lane = threadIdx.x & 63, h = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (h >= c.n_heads) return;
+    const int n = head_rows(c, h), over = rows_over(n, budget[h], w);
     const int64_t newest = (int64_t)pos[h] - w;
-    const int b = max(budget[h], w);
     int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off) + (int64_t)h * p.pairs;
-    int32_t* n_pairs = reinterpret_cast<int32_t*>(ws + p.count_off) + h;
-    // an entry's order, all ones (above every one that may leave) where it may not
-    auto key_of = [&](int r) -> unsigned long long {
-        const int64_t at = pool_row(c, h, r);
-        if (at < 0 || c.idx[at] > newest) return ~0ull;
-        return (unsigned long long)weight_key(c.cum[at]) << 32 | position_key(c.idx[at]);
-    };
-    int may = 0;
-    if (n > b)
-        for (int r = tid; r < n; r += kSelectThreads) {
-            const int64_t at = pool_row(c, h, r);
-            may += at >= 0 && c.idx[at] <= newest;
+    const int32_t* table = c.table + (int64_t)h * c.max_pages;
+    const int in_page = (1 << c.shift) - 1;
+    int drop = 0, gaps = 0;
+    if (over > 0) {
+        int at[R];                                                        // rows of the pool
+        uint32_t key[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int r = 64 * i + lane;
+            at[i] = table[min(r >> c.shift, c.max_pages - 1)];
         }
-    may = block_sum(may, buf);
-    const int drop = n > b ? min(n - b, may) : 0;
-    if (tid == 0) {
-        if (evicted != nullptr) evicted[h] = drop;
-        *n_pairs = 0;
-    }
-    if (drop == 0) return;
-    // the drop-th smallest key: its prefix grows by eight bits a round; `left` of the keys with that prefix leave
-    unsigned long long prefix = 0;
-    int left = drop;
-    for (int bit = 56; bit >= 0; bit -= 8) {
-        for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0;
-        __syncthreads();
-        for (int r = tid; r < n; r += kSelectThreads) {
-            const int64_t at = pool_row(c, h, r);
-            if (at < 0 || c.idx[at] > newest) continue;
-            const unsigned long long k = key_of(r);
-            if (bit == 56 || k >> (bit + 8) == prefix >> (bit + 8)) atomicAdd(&hist[(k >> bit) & 255], 1);
+        int may = 0;
+        unsigned long long lacking = 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int r = 64 * i + lane;
+            const bool there = r < n && page_ok(c, at[i]);
+            lacking |= __ballot(r < n && !there);
+            at[i] = there ? (at[i] << c.shift) + (r & in_page) : 0;
+            const float f = c.cum[at[i]];
+            key[i] = c.idx[at[i]] <= newest ? weight_key(f) : kStays;
+            key[i] = there ? key[i] : kStays;
+            may += __popcll(__ballot(key[i] != kStays));
         }
-        __syncthreads();
-        if (tid == 0) {
-            int sum = 0, d = 0;
-            while (d < 255 && sum + hist[d] < left) sum += hist[d++];
-            pick[0] = d;
-            pick[1] = sum;
-        }
-        __syncthreads();
-        prefix |= (unsigned long long)pick[0] << bit;
-        left -= pick[1];
-        __syncthreads();
-    }
-    // gaps and survivors, in row order
-    const int stay = n - drop;
-    int gaps = 0, movers = 0, equal = 0;
-    for (int r0 = 0; r0 < n; r0 += kSelectThreads) {
-        const int r = r0 + tid;
-        bool leaves = false, same = false;
-        if (r < n) {
-            const int64_t at = pool_row(c, h, r);
-            if (at >= 0 && c.idx[at] <= newest) {
-                const unsigned long long k = key_of(r);
-                leaves = k < prefix;
-                same = k == prefix;
+        drop = lacking != 0 ? 0 : min(over, may);
+        // the largest cut that fewer than `drop` keys lie below: the key of the last to leave.  Where as many as that lie below a cut on
+        // the way, it is one.
+        uint32_t cut = 0;
+        bool exact = false;
+        const auto below = [&](uint32_t x) {
+            int m = 0;
+#pragma unroll
+            for (int i = 0; i < R; ++i) m += __popcll(__ballot(key[i] < x));
+            return m;
+        };
+        int under = 0;
+        if (drop > 0)
+            for (int bit = 31; bit >= 0 && !exact; --bit) {
+                const uint32_t x = cut | 1u << bit;
+                const int m = below(x);
+                if (m <= drop) {
+                    cut = x;
+                    under = m;
+                    exact = m == drop;
+                }
+            }
+        uint32_t leaves = 0;                                              // bit i: row 64 i + lane
+#pragma unroll
+        for (int i = 0; i < R; ++i) leaves |= key[i] < cut ? 1u << i : 0u;
+        if (drop > 0 && !exact) {
+            // keys equal to the cut: all of them, or the lowest positions, or of the last position the first rows
+            int left = drop - under;
+            uint32_t place[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) place[i] = key[i] == cut ? position_key(c.idx[at[i]]) : 0xffffffffu;
+            const auto before = [&](uint32_t x) {
+                int m = 0;
+#pragma unroll
+                for (int i = 0; i < R; ++i) m += __popcll(__ballot(key[i] == cut && place[i] < x));
+                return m;
+            };
+            uint32_t last = 0;
+            int first = 0;
+            for (int bit = 31; bit >= 0; --bit) {
+                const int m = before(last | 1u << bit);
+                if (m < left) {
+                    last |= 1u << bit;
+                    first = m;
+                }
+            }
+            left -= first;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const bool same = key[i] == cut && place[i] == last;
+                const unsigned long long m = __ballot(same);
+                if ((key[i] == cut && place[i] < last) || (same && __popcll(m & ((1ull << lane) - 1)) < left)) leaves |= 1u << i;
+                left -= __popcll(m);
             }
         }
-        int total;
-        const int e = block_scan(same, buf, &total);
-        if (same && equal + e < left) leaves = true;
-        equal += total;
-        const bool gap = leaves && r < stay, mover = r < n && !leaves && r >= stay;
-        const int g = block_scan(gap, buf, &total);
-        if (gap) pairs[gaps + g].x = r;
-        gaps += total;
-        const int m = block_scan(mover, buf, &total);
-        if (mover) pairs[movers + m].y = r;
-        movers += total;
+        const int stay = n - drop;
+        int movers = 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int r = 64 * i + lane;
+            const bool out = leaves >> i & 1, gap = out && r < stay, mover = !out && r >= stay && r < n;
+            const unsigned long long g = __ballot(gap), m = __ballot(mover), lower = (1ull << lane) - 1;
+            if (gap) pairs[gaps + __popcll(g & lower)].x = at[i];
+            if (mover) pairs[movers + __popcll(m & lower)].y = at[i];
+            gaps += __popcll(g);
+            movers += __popcll(m);
+        }
+        if (lane == 0 && drop > 0) c.len[h] = stay;
     }
-    if (tid == 0) {
-        *n_pairs = gaps;
-        c.len[h] = stay;
+    if (lane == 0) {
+        if (evicted != nullptr) evicted[h] = drop;
+        reinterpret_cast<int32_t*>(ws + p.count_off)[h] = gaps;
     }
 }
 
+// Longer tables: a workgroup per head, keys in LDS where they fit (n_keys of them) and from memory otherwise.
+__global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos,
+                                                                      int w, PagedEvictPlan p, char* ws, int32_t* __restrict__ evicted) {
+    extern __shared__ uint32_t key_s[];
+    __shared__ int hist[kSelectThreads];
+    __shared__ int buf[kSelectThreads / 64];
+    __shared__ uint32_t range[2];
+    __shared__ int pick[3];
+    const int h = spread_head(blockIdx.x, gridDim.x), tid = threadIdx.x;
+    const int n = head_rows(c, h), over = rows_over(n, budget[h], w);
+    const int64_t newest = (int64_t)pos[h] - w;
+    int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off) + (int64_t)h * p.pairs;
+    const bool in_lds = n <= p.n_keys;
+    const auto make_key = [&](int64_t at) -> uint32_t {
+        const int64_t from = at >= 0 ? at : 0;
+        const float f = c.cum[from];
+        return at >= 0 && c.idx[from] <= newest ? weight_key(f) : kStays;
+    };
+    const auto key_of = [&](int r) { return in_lds ? key_s[r] : make_key(pool_row(c, h, r)); };
+    int may = 0, lacking = 0;
+    if (over > 0) {
+#pragma unroll 4
+        for (int r = tid; r < n; r += kSelectThreads) {
+            const int64_t at = pool_row(c, h, r);
+            const uint32_t k = make_key(at);
+            if (in_lds) key_s[r] = k;
+            may += k != kStays;
+            lacking += at < 0;
+        }
+        block_scan(may, buf, &may);
+        block_scan(lacking, buf, &lacking);
+    }
+    const int drop = lacking > 0 ? 0 : min(over, may);
+    if (tid == 0) {
+        if (evicted != nullptr) evicted[h] = drop;
+        if (drop == 0) reinterpret_cast<int32_t*>(ws + p.count_off)[h] = 0;
+    }
+    if (drop == 0) return;
+    __syncthreads();
+    int left;
+    const uint32_t cut = last_of_smallest([&](auto&& f) {
+        for (int r = tid; r < n; r += kSelectThreads) {
+            const uint32_t k = key_of(r);
+            if (k != kStays) f(k);
+        }
+    }, drop, hist, buf, range, pick, &left);
+    const bool ties = left != 0x7fffffff;                                 // some of the rows with the last key stay
+    uint32_t last = 0;
+    if (ties)
+        last = last_of_smallest([&](auto&& f) {
+            for (int r = tid; r < n; r += kSelectThreads)
+                if (key_of(r) == cut) f(position_key(c.idx[pool_row(c, h, r)]));
+        }, left, hist, buf, range, pick, &left);
+    // Every thread takes a run of rows behind one another: one scan of the threads' counts says where its gaps and survivors go.
+    const int stay = n - drop, run = (n + kSelectThreads - 1) / kSelectThreads, begin = min(n, tid * run), end = min(n, begin + run);
+    int same = 0;                                                         // rows before the run with the last key and the last position
+    if (ties && left != 0x7fffffff) {
+        for (int r = begin; r < end; ++r) same += key_of(r) == cut && position_key(c.idx[pool_row(c, h, r)]) == last;
+        int total;
+        same = block_scan(same, buf, &total);
+    }
+    const auto each_row = [&](auto&& gap, auto&& mover) {
+        int seen = same;
+        for (int r = begin; r < end; ++r) {
+            const uint32_t k = key_of(r);
+            bool out = k <= cut;
+            if (ties && k == cut) {
+                const uint32_t place = position_key(c.idx[pool_row(c, h, r)]);
+                out = place < last || (place == last && seen++ < left);
+            }
+            if (out && r < stay) gap(r);
+            if (!out && r >= stay) mover(r);
+        }
+    };
+    int gaps = 0, movers = 0, total;
+    each_row([&](int) { ++gaps; }, [&](int) { ++movers; });
+    int to = block_scan(gaps, buf, &total);
+    if (tid == 0) {
+        reinterpret_cast<int32_t*>(ws + p.count_off)[h] = total;
+        c.len[h] = stay;
+    }
+    int from = block_scan(movers, buf, &total);
+    each_row([&](int r) { pairs[to++].x = (int)pool_row(c, h, r); }, [&](int r) { pairs[from++].y = (int)pool_row(c, h, r); });
+}
+
+// Moves the paired rows: 16 bytes a lane of K and of V, four pairs at a time.
 __global__ __launch_bounds__(256) void paged_move_kernel(PagedCache c, int row_size, int n_chunks, PagedEvictPlan p, const char* __restrict__ ws) {
     const int h = blockIdx.x / n_chunks;
     const int2* pairs = reinterpret_cast<const int2*>(ws + p.pair_off) + (int64_t)h * p.pairs;
@@ -641,15 +803,33 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedCache c, int row_s
     const int lanes = row_size / 16, per = 256 / lanes, piece = (threadIdx.x % lanes) * 16;
     char* K = static_cast<char*>(c.K);
     char* V = static_cast<char*>(c.V);
-    for (int i = (blockIdx.x % n_chunks) * per + threadIdx.x / lanes; i < n; i += n_chunks * per) {
-        const int2 m = pairs[i];
-        const int64_t to = pool_row(c, h, m.x), from = pool_row(c, h, m.y);
-        if (to < 0 || from < 0) continue;
-        copy_bytes<16>(K + from * row_size + piece, K + to * row_size + piece);
-        copy_bytes<16>(V + from * row_size + piece, V + to * row_size + piece);
-        if (piece == 0) {
-            c.idx[to] = c.idx[from];
-            c.cum[to] = c.cum[from];
+    constexpr int kAhead = 4;
+    const int step = n_chunks * per;
+    for (int i0 = (blockIdx.x % n_chunks) * per + threadIdx.x / lanes; i0 < n; i0 += kAhead * step) {
+        int2 m[kAhead];
+        uint4 k[kAhead], v[kAhead];
+        int32_t idx[kAhead];
+        float cum[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) m[i] = pairs[min(i0 + i * step, n - 1)];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t from = m[i].y;
+            k[i] = *reinterpret_cast<const uint4*>(K + from * row_size + piece);
+            v[i] = *reinterpret_cast<const uint4*>(V + from * row_size + piece);
+            idx[i] = c.idx[from];
+            cum[i] = c.cum[from];
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (i0 + i * step >= n) continue;
+            const int64_t to = m[i].x;
+            *reinterpret_cast<uint4*>(K + to * row_size + piece) = k[i];
+            *reinterpret_cast<uint4*>(V + to * row_size + piece) = v[i];
+            if (piece == 0) {
+                c.idx[to] = idx[i];
+                c.cum[to] = cum[i];
+            }
         }
     }
 }
@@ -691,6 +871,7 @@ PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows) {
 PagedEvictPlan plan_paged_evict(int n_heads, int rows) {
     PagedEvictPlan p{};
     p.pairs = rows / 2 + 1;
+    p.n_keys = rows < kSelectKeys ? rows : kSelectKeys;
     p.count_off = 0;
     p.pair_off = align_up((size_t)n_heads * sizeof(int32_t), 256);
     p.bytes = p.pair_off + (size_t)n_heads * p.pairs * sizeof(int2);
@@ -765,7 +946,7 @@ hipError_t init_paged_kernels() {
                 });
                 if (e != hipSuccess) return e;
             }
-    return hipSuccess;
+    return allow_dynamic_lds(reinterpret_cast<const void*>(paged_select_kernel), kSelectKeys * sizeof(uint32_t));
 }
 
 hipError_t launch_paged_step(const PagedCache& c, const void* q, const void* k_new, const void* v_new, uncomp_dtype dt, const int32_t* pos, int G,
@@ -778,7 +959,11 @@ hipError_t launch_paged_step(const PagedCache& c, const void* q, const void* k_n
 hipError_t launch_paged_evict(const PagedCache& c, const int32_t* budget, const int32_t* pos, int w, int row_size, const PagedEvictPlan& p, char* ws,
                               int32_t* evicted, const Env& env) {
     env.begin("paged_select");
-    paged_select_kernel<<<c.n_heads, kSelectThreads, 0, env.s>>>(c, budget, pos, w, p, ws, evicted);
+    const int rows = c.max_pages << c.shift;
+    const unsigned by_wave = (unsigned)(c.n_heads + 3) / 4;
+    if (rows <= 64 * 16) paged_select_wave_kernel<16><<<by_wave, 256, 0, env.s>>>(c, budget, pos, w, p, ws, evicted);
+    else if (rows <= 64 * 32) paged_select_wave_kernel<32><<<by_wave, 256, 0, env.s>>>(c, budget, pos, w, p, ws, evicted);
+    else paged_select_kernel<<<c.n_heads, kSelectThreads, p.n_keys * sizeof(uint32_t), env.s>>>(c, budget, pos, w, p, ws, evicted);
     env.end();
     int n_chunks = 2048 / c.n_heads;
     const int most = (p.pairs + 31) / 32;

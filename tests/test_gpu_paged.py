@@ -302,6 +302,38 @@ def test_evict_ties_infinities_and_nothing_old_enough(ctx):
     _check_evict(ctx, c, [100, 23, 30, 10, 10, 1110], [2000, 2000, 2000, 300, 2 ** 31 - 1, 2000], 0)
 
 
+@pytest.mark.parametrize("max_pages", [20, 60, 1200])
+def test_evict_leaves_a_head_that_lacks_a_page(ctx, max_pages):
+    """Tables of up to 1024 rows, up to 2048 and beyond."""
+    lens = [1000, 1000, 1000]
+    c, _ = _cache(ctx, lens, 32 if max_pages > 20 else 64, max_pages, 64, torch.bfloat16, 26)
+    c.table[1, 3] = -1
+    c.length[2] = 10 ** 6                                                # cut to the table's rows, whose later pages are none
+    before = _host(c)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    kept = _rows(c, 0)
+    evicted = ctx.paged_evict(c, i32([100] * 3), i32([10 ** 6] * 3), 4)
+    torch.cuda.synchronize()
+    assert evicted.cpu().tolist() == [900, 0, 0] and c.length.cpu().tolist() == [100, 1000, 10 ** 6]
+    order = O.evict_lowest(kept[3].numpy(), kept[2].numpy(), 100, 10 ** 6, 4)
+    assert np.array_equal(raw_bits(_rows(c, 0)[0]), raw_bits(kept[0][order]))
+    mine = c.table[0, : -(-1000 // c.K.shape[1])].cpu().tolist()
+    others = [p for p in range(c.K.shape[0]) if p not in mine]
+    for a, b in zip(_host(c)[:4], before[:4]):
+        assert np.array_equal(a[others], b[others])
+
+
+def test_evict_keys_over_the_whole_range_of_floats(ctx):
+    """The widest range of keys a search can meet, in tables of every size: negative, tiny, huge, infinite and NaN scores."""
+    g = torch.Generator().manual_seed(27)
+    for lens, max_pages in (([900, 31], 32), ([1900, 2000], 64), ([5000, 2500], 200), ([70000], 2200)):
+        c, _ = _cache(ctx, lens, 32, max_pages, 64, torch.bfloat16, 28)
+        bits = torch.randint(-(2 ** 31), 2 ** 31 - 1, c.cum.shape, generator=g, dtype=torch.int64).to(torch.int32)
+        c.cum.copy_(bits.view(torch.float32))
+        _check_evict(ctx, c, [n // 2 for n in lens], [10 ** 6] * len(lens), 5)
+        _check_evict(ctx, c, [n // 2 - 1 for n in lens], [10 ** 6] * len(lens), 5)
+
+
 @pytest.mark.parametrize("heads,rows", [(2, 50000), (40, 9000), (900, 500)])
 def test_evict_at_length(ctx, heads, rows):
     lens = [rows - (h * 37) % (rows // 2) for h in range(heads)]
