@@ -285,7 +285,8 @@ struct PagedEvictPlan {
     int pairs;           // most rows of one head that move
     size_t count_off;    // int32 [n_heads]
     size_t pair_off;     // int2  [n_heads][pairs]: to, from (rows of the pool)
-    int n_keys;          // keys of a head that the selection holds in LDS
+    int key_rows;        // tables whose keys do not fit in LDS: rows a head has in
+    size_t key_off;      // uint32 [n_heads][key_rows]
     size_t bytes;
 };
 PagedEvictPlan plan_paged_evict(int n_heads, int rows);

@@ -17,7 +17,7 @@ constexpr int kSplitAim = 768;                        // workgroups of the atten
 // One workgroup a head: from as many heads on as fill the chip, with logits that leave room for two workgroups on a CU.
 constexpr int kHeadLaunchHeads = 512;
 constexpr size_t kHeadLaunchLds = 76 * 1024;
-constexpr int kSelectThreads = 1024, kSelectKeys = 32768;         // threads of a selection, keys that it holds in LDS
+constexpr int kSelectThreads = 1024, kSelectKeys = 32768, kWaveSelectHeads = 512;      // threads of a selection, keys that it holds in LDS
 
 __device__ __forceinline__ int head_rows(const PagedCache& c, int h) {
     const int cap = c.max_pages << c.shift;
@@ -511,9 +511,15 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache
 // done with their positions, and with equal positions in row order.  The i-th gap before the new end is then paired with the i-th survivor
 // behind it, as rows of the pool, and another kernel moves the rows.
 namespace {
-constexpr uint32_t kStays = 0xffffffffu;                // the key of a row that may not leave: above every other
+constexpr uint32_t kStays = 0xffffffffu, kLacks = kStays - 1;      // the keys of a row that may not leave, and of one without a page: above every other
 
-__device__ __forceinline__ uint32_t weight_key(float f) { return f != f ? kStays - 1 : order_key(f); }
+__device__ __forceinline__ uint32_t weight_key(float f) { return f != f ? kLacks - 1 : order_key(f); }
+__device__ __forceinline__ uint32_t row_key(const PagedCache& c, int64_t at, int64_t newest) {
+    const int64_t from = at >= 0 ? at : 0;
+    const float f = c.cum[from];
+    const int32_t place = c.idx[from];
+    return at < 0 ? kLacks : place <= newest ? weight_key(f) : kStays;
+}
 __device__ __forceinline__ uint32_t position_key(int32_t p) { return (uint32_t)p ^ 0x80000000u; }
 
 // how many rows a head has to give up, were they all old enough
@@ -544,11 +550,77 @@ __device__ __forceinline__ int block_scan(int v, int* buf, int* total) {
     return before + s - v;
 }
 
-// The `want` smallest of the keys that each(f) hands to f, by a histogram of 1024 bins over what is left of their range, ten bits a
-// round (the workgroup's threads together; at least `want` keys).  Returns the key of the last of them; *left: how many
-// keys equal to it are among them (INT_MAX: all).
+// The `want` smallest of the keys that each(f) hands to f (at least `want`): a histogram over what is left of their range, its bin that holds
+// the last of them the next range.  cut: the key of the last; left: how many keys equal to it are among them (INT_MAX: all).
+struct Cut {
+    uint32_t key;
+    int left;
+};
+constexpr int kAll = 0x7fffffff;
+// the round's end, the same for whoever searches: `before` keys lie below bin `bin` of 1 << shift, `here` in it
+__device__ __forceinline__ bool narrow(uint32_t& lo, uint32_t& hi, int shift, int bin, int before, int here, int& want, Cut* cut) {
+    want -= before;
+    lo += (uint32_t)bin << shift;
+    if (hi - lo >= 1u << shift) hi = lo + ((1u << shift) - 1u);
+    *cut = Cut{hi, here == want ? kAll : want};
+    return here == want || shift == 0;
+}
+__device__ __forceinline__ int shift_of(uint32_t lo, uint32_t hi, int bits) {
+    const int n = hi == lo ? 0 : 32 - __clz((int)(hi - lo));
+    return n > bits ? n - bits : 0;
+}
+
+// by one wave: 256 bins of its own in LDS, four a lane
 template <typename F>
-__device__ uint32_t last_of_smallest(F&& each, int want, int* hist, int* buf, uint32_t* range, int* pick, int* left) {
+__device__ __forceinline__ Cut last_of_smallest_wave(F&& each, int want, int* hist) {
+    const int lane = threadIdx.x & 63;
+    const auto in_order = []() {                                          // a wave's LDS instructions run in order; the compiler's too, from here to there
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
+    uint32_t lo = 0xffffffffu, hi = 0u;
+    each([&](uint32_t k) {
+        lo = min(lo, k);
+        hi = max(hi, k);
+    });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+    }
+    Cut cut;
+    while (true) {
+        const int shift = shift_of(lo, hi, 8);
+        reinterpret_cast<int4*>(hist)[lane] = make_int4(0, 0, 0, 0);
+        in_order();
+        each([&](uint32_t k) {
+            if (k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1);
+        });
+        in_order();
+        const int4 h = reinterpret_cast<const int4*>(hist)[lane];
+        const int mine = (h.x + h.y) + (h.z + h.w);
+        int sum = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += u;
+        }
+        // the lane whose four bins hold the want-th key, and the bin among them
+        const int x = __ffsll(__ballot(sum >= want)) - 1;
+        int before = sum - mine, bin = 4 * lane, here = h.x;
+        if (before + here < want) { before += here; here = h.y; ++bin; }
+        if (before + here < want) { before += here; here = h.z; ++bin; }
+        if (before + here < want) { before += here; here = h.w; ++bin; }
+        if (narrow(lo, hi, shift, __builtin_amdgcn_readlane(bin, x), __builtin_amdgcn_readlane(before, x), __builtin_amdgcn_readlane(here, x), want, &cut))
+            return cut;
+        in_order();
+    }
+}
+
+// by the workgroup: a bin a thread
+template <typename F>
+__device__ Cut last_of_smallest(F&& each, int want, int* hist, int* buf, uint32_t* range, int* pick) {
     const int tid = threadIdx.x;
     uint32_t lo = 0xffffffffu, hi = 0u;
     each([&](uint32_t k) {
@@ -572,8 +644,9 @@ __device__ uint32_t last_of_smallest(F&& each, int want, int* hist, int* buf, ui
     __syncthreads();
     lo = range[0];
     hi = range[1];
+    Cut cut;
     while (true) {
-        const int bits = hi == lo ? 0 : 32 - __clz((int)(hi - lo)), shift = bits > 10 ? bits - 10 : 0;
+        const int shift = shift_of(lo, hi, 10);
         hist[tid] = 0;
         __syncthreads();
         each([&](uint32_t k) {
@@ -588,27 +661,23 @@ __device__ uint32_t last_of_smallest(F&& each, int want, int* hist, int* buf, ui
             pick[2] = here;
         }
         __syncthreads();
-        want -= pick[1];
-        lo += (uint32_t)pick[0] << shift;
-        if (hi - lo >= 1u << shift) hi = lo + ((1u << shift) - 1u);
-        const bool all = pick[2] == want;
+        const bool done = narrow(lo, hi, shift, pick[0], pick[1], pick[2], want, &cut);
         __syncthreads();
-        if (all || shift == 0) {
-            *left = all ? 0x7fffffff : want;
-            return hi;
-        }
+        if (done) return cut;
     }
 }
 }  // namespace
 
-// Short tables (at most 64 R rows): a wave per head, every row's key in a register, the cut found bit by bit with a count of the
-// keys below it; no workgroup has to wait for anything.
+// Short tables (at most 64 R rows): a wave per head with every row's key in a register; nobody waits for anybody.  Whole evictions, us: 5120 heads
+// of 720 rows, an eighth of them without weight, 150 (274 with the cut found bit by bit, by counts of the keys below it).  By a wave and by
+// a workgroup per head: 8 heads of 1900 rows 46 / 29, 256 heads 62 / 48, 2000 heads 116 / 202.
 template <int R>
 __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos,
                                                                 int w, PagedEvictPlan p, char* ws, int32_t* __restrict__ evicted) {
-    const int lane = threadIdx.x & 63, h = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    if (h >= c.n_heads) return;
-    const int n = head_rows(c, h), over = rows_over(n, budget[h], w);
+    __shared__ __align__(16) int hist_s[4][256];
+    const int lane = threadIdx.x & 63, wg = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (wg >= c.n_heads) return;
+    const int h = spread_head(wg, c.n_heads), n = head_rows(c, h), over = rows_over(n, budget[h], w);
     const int64_t newest = (int64_t)pos[h] - w;
     int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off) + (int64_t)h * p.pairs;
     const int32_t* table = c.table + (int64_t)h * c.max_pages;
@@ -636,58 +705,33 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
             may += __popcll(__ballot(key[i] != kStays));
         }
         drop = lacking != 0 ? 0 : min(over, may);
-        // the largest cut that fewer than `drop` keys lie below: the key of the last to leave.  Where as many as that lie below a cut on
-        // the way, it is one.
-        uint32_t cut = 0;
-        bool exact = false;
-        const auto below = [&](uint32_t x) {
-            int m = 0;
-#pragma unroll
-            for (int i = 0; i < R; ++i) m += __popcll(__ballot(key[i] < x));
-            return m;
-        };
-        int under = 0;
-        if (drop > 0)
-            for (int bit = 31; bit >= 0 && !exact; --bit) {
-                const uint32_t x = cut | 1u << bit;
-                const int m = below(x);
-                if (m <= drop) {
-                    cut = x;
-                    under = m;
-                    exact = m == drop;
-                }
-            }
         uint32_t leaves = 0;                                              // bit i: row 64 i + lane
+        if (drop > 0) {
+            int* hist = hist_s[threadIdx.x >> 6];
+            Cut cut = last_of_smallest_wave([&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) leaves |= key[i] < cut ? 1u << i : 0u;
-        if (drop > 0 && !exact) {
-            // keys equal to the cut: all of them, or the lowest positions, or of the last position the first rows
-            int left = drop - under;
-            uint32_t place[R];
+                for (int i = 0; i < R; ++i)
+                    if (key[i] != kStays) f(key[i]);
+            }, drop, hist);
 #pragma unroll
-            for (int i = 0; i < R; ++i) place[i] = key[i] == cut ? position_key(c.idx[at[i]]) : 0xffffffffu;
-            const auto before = [&](uint32_t x) {
-                int m = 0;
+            for (int i = 0; i < R; ++i) leaves |= key[i] < cut.key || (cut.left == kAll && key[i] == cut.key) ? 1u << i : 0u;
+            if (cut.left != kAll) {
+                // of the rows with the last key the lowest positions, of those at the last position the first rows
+                uint32_t place[R];
 #pragma unroll
-                for (int i = 0; i < R; ++i) m += __popcll(__ballot(key[i] == cut && place[i] < x));
-                return m;
-            };
-            uint32_t last = 0;
-            int first = 0;
-            for (int bit = 31; bit >= 0; --bit) {
-                const int m = before(last | 1u << bit);
-                if (m < left) {
-                    last |= 1u << bit;
-                    first = m;
+                for (int i = 0; i < R; ++i) place[i] = key[i] == cut.key ? position_key(c.idx[at[i]]) : 0u;
+                Cut last = last_of_smallest_wave([&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int i = 0; i < R; ++i)
+                        if (key[i] == cut.key) f(place[i]);
+                }, cut.left, hist);
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    const bool tied = key[i] == cut.key, same = tied && place[i] == last.key;
+                    const unsigned long long m = __ballot(same);
+                    if ((tied && place[i] < last.key) || (same && __popcll(m & ((1ull << lane) - 1)) < last.left)) leaves |= 1u << i;
+                    if (last.left != kAll) last.left -= __popcll(m);
                 }
-            }
-            left -= first;
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const bool same = key[i] == cut && place[i] == last;
-                const unsigned long long m = __ballot(same);
-                if ((key[i] == cut && place[i] < last) || (same && __popcll(m & ((1ull << lane) - 1)) < left)) leaves |= 1u << i;
-                left -= __popcll(m);
             }
         }
         const int stay = n - drop;
@@ -710,10 +754,25 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
     }
 }
 
-// Longer tables: a workgroup per head, keys in LDS where they fit (n_keys of them) and from memory otherwise.
+// Keys of tables that do not fit in LDS, made by as many workgroups as there are: 1024 rows each.
+__global__ __launch_bounds__(256) void paged_key_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos, int w,
+                                                        PagedEvictPlan p, int n_chunks, char* ws) {
+    const int h = blockIdx.x / n_chunks, n = head_rows(c, h);
+    if (rows_over(n, budget[h], w) == 0) return;
+    const int64_t newest = (int64_t)pos[h] - w;
+    uint32_t* key = reinterpret_cast<uint32_t*>(ws + p.key_off) + (int64_t)h * p.key_rows;
+    const int first = blockIdx.x % n_chunks * 1024 + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = first + 256 * i;
+        if (r < n) key[r] = row_key(c, pool_row(c, h, r), newest);
+    }
+}
+
+// Longer tables: a workgroup per head, keys in LDS where they fit and from the workspace otherwise, four at a time.
 __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos,
                                                                       int w, PagedEvictPlan p, char* ws, int32_t* __restrict__ evicted) {
-    extern __shared__ uint32_t key_s[];
+    extern __shared__ __align__(16) uint32_t key_s[];
     __shared__ int hist[kSelectThreads];
     __shared__ int buf[kSelectThreads / 64];
     __shared__ uint32_t range[2];
@@ -722,23 +781,30 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache
     const int n = head_rows(c, h), over = rows_over(n, budget[h], w);
     const int64_t newest = (int64_t)pos[h] - w;
     int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off) + (int64_t)h * p.pairs;
-    const bool in_lds = n <= p.n_keys;
-    const auto make_key = [&](int64_t at) -> uint32_t {
-        const int64_t from = at >= 0 ? at : 0;
-        const float f = c.cum[from];
-        return at >= 0 && c.idx[from] <= newest ? weight_key(f) : kStays;
+    const bool in_lds = p.key_rows == 0;
+    const uint32_t* key_m = reinterpret_cast<const uint32_t*>(ws + p.key_off) + (int64_t)h * p.key_rows;
+    if (in_lds && over > 0) {
+#pragma unroll 4
+        for (int r = tid; r < n; r += kSelectThreads) key_s[r] = row_key(c, pool_row(c, h, r), newest);
+        __syncthreads();
+    }
+    const auto four = [&](int r) { return in_lds ? *reinterpret_cast<const uint4*>(key_s + r) : *reinterpret_cast<const uint4*>(key_m + r); };
+    // f(row, key) of every row from `begin` to `end`, `step` rows between fours
+    const auto each_key = [&](int begin, int end, int step, auto&& f) __attribute__((always_inline)) {
+        for (int r = begin; r < end; r += step) {
+            const uint4 k = four(r);
+            f(r, k.x);
+            if (r + 1 < end) f(r + 1, k.y);
+            if (r + 2 < end) f(r + 2, k.z);
+            if (r + 3 < end) f(r + 3, k.w);
+        }
     };
-    const auto key_of = [&](int r) { return in_lds ? key_s[r] : make_key(pool_row(c, h, r)); };
     int may = 0, lacking = 0;
     if (over > 0) {
-#pragma unroll 4
-        for (int r = tid; r < n; r += kSelectThreads) {
-            const int64_t at = pool_row(c, h, r);
-            const uint32_t k = make_key(at);
-            if (in_lds) key_s[r] = k;
-            may += k != kStays;
-            lacking += at < 0;
-        }
+        each_key(4 * tid, n, 4 * kSelectThreads, [&](int, uint32_t k) {
+            may += k < kLacks;
+            lacking += k == kLacks;
+        });
         block_scan(may, buf, &may);
         block_scan(lacking, buf, &lacking);
     }
@@ -749,40 +815,39 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache
     }
     if (drop == 0) return;
     __syncthreads();
-    int left;
-    const uint32_t cut = last_of_smallest([&](auto&& f) {
-        for (int r = tid; r < n; r += kSelectThreads) {
-            const uint32_t k = key_of(r);
-            if (k != kStays) f(k);
-        }
-    }, drop, hist, buf, range, pick, &left);
-    const bool ties = left != 0x7fffffff;                                 // some of the rows with the last key stay
-    uint32_t last = 0;
+    const Cut cut = last_of_smallest([&](auto&& f) {
+        each_key(4 * tid, n, 4 * kSelectThreads, [&](int, uint32_t k) {
+            if (k < kLacks) f(k);
+        });
+    }, drop, hist, buf, range, pick);
+    const bool ties = cut.left != kAll;                                   // some of the rows with the last key stay
+    const auto place_of = [&](int r) { return position_key(c.idx[pool_row(c, h, r)]); };
+    Cut last{0u, kAll};
     if (ties)
         last = last_of_smallest([&](auto&& f) {
-            for (int r = tid; r < n; r += kSelectThreads)
-                if (key_of(r) == cut) f(position_key(c.idx[pool_row(c, h, r)]));
-        }, left, hist, buf, range, pick, &left);
+            each_key(4 * tid, n, 4 * kSelectThreads, [&](int r, uint32_t k) {
+                if (k == cut.key) f(place_of(r));
+            });
+        }, cut.left, hist, buf, range, pick);
     // Every thread takes a run of rows behind one another: one scan of the threads' counts says where its gaps and survivors go.
-    const int stay = n - drop, run = (n + kSelectThreads - 1) / kSelectThreads, begin = min(n, tid * run), end = min(n, begin + run);
+    const int stay = n - drop, run = ((n + kSelectThreads - 1) / kSelectThreads + 3) & ~3, begin = min(n, tid * run), end = min(n, begin + run);
     int same = 0;                                                         // rows before the run with the last key and the last position
-    if (ties && left != 0x7fffffff) {
-        for (int r = begin; r < end; ++r) same += key_of(r) == cut && position_key(c.idx[pool_row(c, h, r)]) == last;
+    if (last.left != kAll) {
+        each_key(begin, end, 4, [&](int r, uint32_t k) { same += k == cut.key && place_of(r) == last.key; });
         int total;
         same = block_scan(same, buf, &total);
     }
-    const auto each_row = [&](auto&& gap, auto&& mover) {
+    const auto each_row = [&](auto&& gap, auto&& mover) __attribute__((always_inline)) {
         int seen = same;
-        for (int r = begin; r < end; ++r) {
-            const uint32_t k = key_of(r);
-            bool out = k <= cut;
-            if (ties && k == cut) {
-                const uint32_t place = position_key(c.idx[pool_row(c, h, r)]);
-                out = place < last || (place == last && seen++ < left);
+        each_key(begin, end, 4, [&](int r, uint32_t k) {
+            bool out = k <= cut.key;
+            if (ties && k == cut.key) {
+                const uint32_t place = place_of(r);
+                out = place < last.key || (place == last.key && seen++ < last.left);
             }
             if (out && r < stay) gap(r);
             if (!out && r >= stay) mover(r);
-        }
+        });
     };
     int gaps = 0, movers = 0, total;
     each_row([&](int) { ++gaps; }, [&](int) { ++movers; });
@@ -797,7 +862,7 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache
 
 // Moves the paired rows: 16 bytes a lane of K and of V, four pairs at a time.
 __global__ __launch_bounds__(256) void paged_move_kernel(PagedCache c, int row_size, int n_chunks, PagedEvictPlan p, const char* __restrict__ ws) {
-    const int h = blockIdx.x / n_chunks;
+    const int h = spread_head(blockIdx.x / n_chunks, c.n_heads);
     const int2* pairs = reinterpret_cast<const int2*>(ws + p.pair_off) + (int64_t)h * p.pairs;
     const int n = reinterpret_cast<const int32_t*>(ws + p.count_off)[h];
     const int lanes = row_size / 16, per = 256 / lanes, piece = (threadIdx.x % lanes) * 16;
@@ -871,10 +936,11 @@ PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows) {
 PagedEvictPlan plan_paged_evict(int n_heads, int rows) {
     PagedEvictPlan p{};
     p.pairs = rows / 2 + 1;
-    p.n_keys = rows < kSelectKeys ? rows : kSelectKeys;
+    p.key_rows = rows > kSelectKeys ? (rows + 3) & ~3 : 0;
     p.count_off = 0;
     p.pair_off = align_up((size_t)n_heads * sizeof(int32_t), 256);
-    p.bytes = p.pair_off + (size_t)n_heads * p.pairs * sizeof(int2);
+    p.key_off = align_up(p.pair_off + (size_t)n_heads * p.pairs * sizeof(int2), 256);
+    p.bytes = p.key_off + (size_t)n_heads * p.key_rows * sizeof(uint32_t);
     return p;
 }
 
@@ -961,9 +1027,21 @@ hipError_t launch_paged_evict(const PagedCache& c, const int32_t* budget, const 
     env.begin("paged_select");
     const int rows = c.max_pages << c.shift;
     const unsigned by_wave = (unsigned)(c.n_heads + 3) / 4;
-    if (rows <= 64 * 16) paged_select_wave_kernel<16><<<by_wave, 256, 0, env.s>>>(c, budget, pos, w, p, ws, evicted);
-    else if (rows <= 64 * 32) paged_select_wave_kernel<32><<<by_wave, 256, 0, env.s>>>(c, budget, pos, w, p, ws, evicted);
-    else paged_select_kernel<<<c.n_heads, kSelectThreads, p.n_keys * sizeof(uint32_t), env.s>>>(c, budget, pos, w, p, ws, evicted);
+    const auto wave_form = [&](auto r) {
+        paged_select_wave_kernel<decltype(r)::value><<<by_wave, 256, 0, env.s>>>(c, budget, pos, w, p, ws, evicted);
+    };
+    const int least = c.n_heads > kWaveSelectHeads ? 64 * 32 : 64 * 16;   // rows up to which a wave per head is the faster form
+    if (rows <= 64 * 8) wave_form(std::integral_constant<int, 8>{});
+    else if (rows <= 64 * 16) wave_form(std::integral_constant<int, 16>{});
+    else if (rows <= 64 * 24 && rows <= least) wave_form(std::integral_constant<int, 24>{});
+    else if (rows <= 64 * 32 && rows <= least) wave_form(std::integral_constant<int, 32>{});
+    else {
+        if (p.key_rows > 0) {
+            const int n_chunks = (rows + 1023) / 1024;
+            paged_key_kernel<<<c.n_heads * n_chunks, 256, 0, env.s>>>(c, budget, pos, w, p, n_chunks, ws);
+        }
+        paged_select_kernel<<<c.n_heads, kSelectThreads, p.key_rows > 0 ? 0 : (size_t)(rows + 3) / 4 * 16, env.s>>>(c, budget, pos, w, p, ws, evicted);
+    }
     env.end();
     int n_chunks = 2048 / c.n_heads;
     const int most = (p.pairs + 31) / 32;
