@@ -14,6 +14,7 @@ namespace {
 constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / 64;
 constexpr int kFinishThreads = 256, kFinishRows = 1024;
 constexpr int kSplitAim = 768;                        // workgroups of the attention of few heads: three a CU
+constexpr int kLeastShare = 128;                      // rows of a workgroup, at least: a block a wave
 // One workgroup a head: from as many heads on as fill the chip, with logits that leave room for two workgroups on a CU.
 constexpr int kHeadLaunchHeads = 512;
 constexpr size_t kHeadLaunchLds = 76 * 1024;
@@ -323,21 +324,21 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_head_kernel(PagedCach
     }
 }
 
-// Few heads: their rows are dealt to about as many workgroups as run at a time, whatever the heads' lengths: `unit` rows each, the last
-// of a head fewer.  Workgroup number -> head and part, from the lengths, 64 of them at a time.
+// Few heads: their rows are dealt to about as many workgroups as run at a time, whatever the heads' lengths: as many parts of a head as it has
+// shares of all rows, begun ones included, and all of one size.  Workgroup number -> head and part, from the lengths, 64 of them at a time.
 struct HeadPart {
-    int h, part, n_parts, unit;
+    int h, part, n_parts;
 };
-__device__ __forceinline__ bool find_head_part(const PagedCache& c, int step, const PagedStepPlan& p, int wg, HeadPart* out) {
+__device__ __forceinline__ bool find_head_part(const PagedCache& c, const PagedStepPlan& p, int wg, HeadPart* out) {
     const int lane = threadIdx.x & 63;
     int64_t total = 0;
     for (int h = lane; h < c.n_heads; h += 64) total += head_rows(c, h) + 1;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
-    const int unit = (int)(((total + p.n_split - 1) / p.n_split + step - 1) / step * step);
-    out->unit = unit;
+    int share = max(kLeastShare, (int)((total + p.n_split - 1) / p.n_split));
+    if (share < 4 * kLeastShare) share = (share + kLeastShare - 1) / kLeastShare * kLeastShare;      // as many blocks for every wave, where they are few
     for (int h0 = 0; h0 < c.n_heads; h0 += 64) {
-        const int parts = h0 + lane < c.n_heads ? head_rows(c, h0 + lane) / unit + 1 : 0;      // a head without rows has one too
+        const int parts = h0 + lane < c.n_heads ? head_rows(c, h0 + lane) / share + 1 : 0;
         int sum = parts;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -370,17 +371,18 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_attend_kernel(PagedCa
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, j = lane >> 4;
     constexpr int kStep = A::kBlock * kAttendWaves;
     HeadPart hp;
-    if (!find_head_part(c, kStep, p, blockIdx.x, &hp)) return;
+    if (!find_head_part(c, p, blockIdx.x, &hp)) return;
     const int h = hp.h;
     A a;
     a.reset();
     a.load_query(col < G ? q + ((int64_t)h * G + col) * D : nullptr, lane);
     const HeadRows hr = rows_of_head(c, h, k_new != nullptr);
-    const int begin = hp.part * hp.unit, end = begin + hp.unit, blocks = hr.n / A::kBlock;
+    const int size = (hr.n / hp.n_parts + A::kBlock) / A::kBlock * A::kBlock;                 // whole blocks, together more than n rows
+    const int begin = hp.part * size, end = begin + size, blocks = hr.n / A::kBlock;
     const bool tail = hr.n1 > blocks * A::kBlock && blocks * A::kBlock >= begin && blocks * A::kBlock < end;
     float* logits = reinterpret_cast<float*>(ws + p.logit_off) + (int64_t)h * GT * p.rows;
     attend_rows<T, D>(a, c, h, hr, k_new + (int64_t)h * D, v_new + (int64_t)h * D, begin + A::kBlock * wave, kStep, min(end, blocks * A::kBlock),
-                      tail && blocks % kAttendWaves == wave, lane, [&](int r, const float (&s)[A::kPerLane]) {
+                      tail && (blocks - begin / A::kBlock) % kAttendWaves == wave, lane, [&](int r, const float (&s)[A::kPerLane]) {
         // a wave's logits change places in LDS (in the order its instructions have there) for stores of whole pieces of 16 bytes
         float* mine = line_s[wave];
         if (col < GT)
@@ -914,7 +916,7 @@ PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows) {
     p.rows = (rows + 31) / 32 * 32;                                       // whole blocks are written
     p.one_launch = n_heads >= kHeadLaunchHeads && head_step_lds(G, D, p.rows) <= kHeadLaunchLds;
     if (p.one_launch) return p;
-    const int64_t units = (int64_t)n_heads * ((rows + 127) / 128);         // of the fewest rows
+    const int64_t units = (int64_t)n_heads * ((rows + kLeastShare - 1) / kLeastShare);
     // broken parts count half: together about as many as run at a time; of more heads than that, several rounds
     const int aim = n_heads < kHeadLaunchHeads ? kSplitAim - n_heads / 2 : 4 * kSplitAim;
     p.n_split = (int)(units < aim ? units : aim);
