@@ -87,6 +87,8 @@ struct WaveAttend<bf16_bits, D> {
             q[s] = __builtin_bit_cast(bf16x8_t, w);
         }
     }
+    // feature of product t that row i of its outputs is (t a multiple of four: of the four products from t on, four features on)
+    static __device__ __forceinline__ int feature(int i, int t) { return kVw * i + t; }
     static __device__ __forceinline__ int key_row(int lane, int tile) { return 16 * tile + row_of(lane & 3, (lane & 15) >> 2); }
     static __device__ __forceinline__ int value_row(int lane, int e) { return 16 * (e >> 2) + row_of(e & 3, lane >> 4); }
     // tile0, tile1: the first rows of the block's two tiles
@@ -183,6 +185,8 @@ struct WaveAttend<float, D> {
         for (int s = 0; s < kSteps; ++s)
             q[s] = qrow != nullptr ? *reinterpret_cast<const f32x4_t*>(qrow + 16 * s + 4 * (lane >> 4)) : f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
+    // sixteen lanes load 256 bytes of a row behind one another
+    static __device__ __forceinline__ int feature(int i, int t) { return 64 * (t >> 2) + 4 * i + (t & 3); }
     static __device__ __forceinline__ int key_row(int lane, int) { return row_of(lane & 3, (lane & 15) >> 2); }
     static __device__ __forceinline__ int value_row(int lane, int e) { return row_of(e, lane >> 4); }
     static __device__ __forceinline__ void load_key(Keys& k, int lane, const float* row) {
@@ -195,7 +199,7 @@ struct WaveAttend<float, D> {
     // e: which of the lane's rows
     static __device__ __forceinline__ void load_value(Values& v, int lane, int e, const float* row) {
 #pragma unroll
-        for (int i = 0; i < kVw / 4; ++i) v.w[e][i] = *reinterpret_cast<const f32x4_t*>(row + kVw * (lane & 15) + 4 * i);
+        for (int i = 0; i < kVw / 4; ++i) v.w[e][i] = *reinterpret_cast<const f32x4_t*>(row + feature(lane & 15, 4 * i));
     }
     static __device__ __forceinline__ void load_values(Values& v, int lane, const float* tile0, const float*) {
 #pragma unroll
@@ -212,7 +216,7 @@ struct WaveAttend<float, D> {
     static __device__ __forceinline__ void put_value(Values& v, int lane, int at, const float* row) {
 #pragma unroll
         for (int i = 0; i < kVw / 4; ++i) {
-            const f32x4_t w = *reinterpret_cast<const f32x4_t*>(row + kVw * (lane & 15) + 4 * i);
+            const f32x4_t w = *reinterpret_cast<const f32x4_t*>(row + feature(lane & 15, 4 * i));
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -232,13 +236,13 @@ struct WaveAttend<float, D> {
         for (int i = 0; i < kVw / 4; ++i) v.w[e][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     __device__ __forceinline__ void logits(const Keys& k, float scale2, float (&s)[kPerLane]) const {
-        f32x4_t c = {0.f, 0.f, 0.f, 0.f};
+        f32x4_t c[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};        // two chains of products
 #pragma unroll
         for (int t = 0; t < kSteps; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(k.w[t][e], q[t][e], c, 0, 0, 0);
+            for (int e = 0; e < 4; ++e) c[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.w[t][e], q[t][e], c[e & 1], 0, 0, 0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = c[e] * scale2;
+        for (int e = 0; e < 4; ++e) s[e] = (c[0][e] + c[1][e]) * scale2;
     }
     __device__ __forceinline__ void add_values(const Values& v, const float (&p)[kPerLane]) {
 #pragma unroll

@@ -307,7 +307,7 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_head_kernel(PagedCach
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int t = 0; t < A::kVw; t += 4)
-                *reinterpret_cast<f32x4_t*>(dyn + (wave * G + col) * D + A::kVw * (4 * j + i) + t) =
+                *reinterpret_cast<f32x4_t*>(dyn + (wave * G + col) * D + A::feature(4 * j + i, t)) =
                     f32x4_t{a.o[t][i] * f, a.o[t + 1][i] * f, a.o[t + 2][i] * f, a.o[t + 3][i] * f};
     }
     __syncthreads();
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_attend_kernel(PagedCa
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int t = 0; t < A::kVw; t += 4)
-                *reinterpret_cast<f32x4_t*>(o_s + (wave * G + col) * D + A::kVw * (4 * j + i) + t) =
+                *reinterpret_cast<f32x4_t*>(o_s + (wave * G + col) * D + A::feature(4 * j + i, t)) =
                     f32x4_t{a.o[t][i] * f, a.o[t + 1][i] * f, a.o[t + 2][i] * f, a.o[t + 3][i] * f};
     }
     if (threadIdx.x < (unsigned)G) {

@@ -204,11 +204,28 @@ __global__ __launch_bounds__(256) void prefill_f32_kernel(PrefillArgs a) {
     at.load_query(Q, lane);
     typename A::Keys keys;
     typename A::Values values;
-    const auto fetch_keys = [&](int r0) { A::load_key(keys, lane, K + min(r0 + A::key_row(lane, 0), w.keys - 1) * a.k.sr); };
+    // a block's first row is uniform, the lane's rows 32-bit offsets from there; behind the last row that one is read again
+    const int k_row = A::key_row(lane, 0), k_at = k_row * (int)a.k.sr;
+    int v_at[A::kPerLane];
+#pragma unroll
+    for (int e = 0; e < A::kPerLane; ++e) v_at[e] = A::value_row(lane, e) * (int)a.v.sr;
+    const auto fetch_keys = [&](int r0) __attribute__((always_inline)) {
+        const float* first = K + (int64_t)min(r0, w.keys - 1) * a.k.sr;
+        if (r0 + A::kBlock <= w.keys) A::load_key(keys, lane, first + k_at);
+        else A::load_key(keys, lane, first + max(0, min(k_row, w.keys - 1 - r0)) * (int)a.k.sr);
+    };
+    const auto fetch_values = [&](int r0) __attribute__((always_inline)) {
+        const float* first = V + (int64_t)r0 * a.v.sr;
+        if (r0 + A::kBlock <= w.keys)
+#pragma unroll
+            for (int e = 0; e < A::kPerLane; ++e) A::load_value(values, lane, e, first + v_at[e]);
+        else
+#pragma unroll
+            for (int e = 0; e < A::kPerLane; ++e) A::load_value(values, lane, e, first + min(A::value_row(lane, e), w.keys - 1 - r0) * (int)a.v.sr);
+    };
     if (end > 0) fetch_keys(0);
     for (int r0 = 0; r0 < end; r0 += A::kBlock) {
-#pragma unroll
-        for (int e = 0; e < A::kPerLane; ++e) A::load_value(values, lane, e, V + min(r0 + A::value_row(lane, e), w.keys - 1) * a.v.sr);
+        fetch_values(r0);
         float p[A::kPerLane];
         at.logits(keys, scale2, p);
         fetch_keys(r0 + A::kBlock);
@@ -233,7 +250,7 @@ __global__ __launch_bounds__(256) void prefill_f32_kernel(PrefillArgs a) {
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int t = 0; t < A::kVw; t += 4)
-                *reinterpret_cast<f32x4_t*>(acc + A::kVw * (4 * j + i) + t) = f32x4_t{at.o[t][i], at.o[t + 1][i], at.o[t + 2][i], at.o[t + 3][i]};
+                *reinterpret_cast<f32x4_t*>(acc + A::feature(4 * j + i, t)) = f32x4_t{at.o[t][i], at.o[t + 1][i], at.o[t + 2][i], at.o[t + 3][i]};
         if (j == 0) a.part_ml[row] = make_float2(at.m, l);
         return;
     }
@@ -243,7 +260,7 @@ __global__ __launch_bounds__(256) void prefill_f32_kernel(PrefillArgs a) {
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int t = 0; t < A::kVw; t += 4)
-            *reinterpret_cast<f32x4_t*>(O + A::kVw * (4 * j + i) + t) =
+            *reinterpret_cast<f32x4_t*>(O + A::feature(4 * j + i, t)) =
                 f32x4_t{at.o[t][i] * inv, at.o[t + 1][i] * inv, at.o[t + 2][i] * inv, at.o[t + 3][i] * inv};
     if (a.lse != nullptr && j == 0)
         a.lse[w.s * a.lse_ss + head * a.lse_sh + w.q_first + qi] = l == 0.f ? -INFINITY : (at.m + log2f(l)) * kLn2A;
@@ -320,7 +337,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const bf16_bits* fir
 }  // namespace
 
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void prefill_tile_kernel(PrefillArgs a) {
+__global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(PrefillArgs a) {
     constexpr int kThreads = 64 * NW, kCols = 32 * NW, kRowBytes = D * 2, kPieces = D / 8, kTileBytes = kTileKeys * kRowBytes;
     constexpr int kMine = kTileKeys * kPieces / kThreads, kSteps = D / 16, kBlocks = D / 32;
     __shared__ __align__(16) unsigned char lds[2][2][kTileBytes];        // [buffer][keys, values]
@@ -578,7 +595,7 @@ Plan plan(bool f32, bool packed, int n_seq, int H, int G, int D, int q_rows, int
     const int64_t cols = (int64_t)q_rows * G;
     Plan p;
     p.tile = f32 ? kWaveCols : D == 64 ? 128 : 256;
-    p.target = p.tile == 256 ? 256 : 512;                                 // workgroups that run at a time
+    p.target = p.tile == 256 ? 256 : f32 ? 512 : 768;                                 // workgroups that run at a time
     p.least = f32 ? kLeastBlocksF32 : kLeastBlocks;
     // most tiles that the sequences can have: whole ones, and one broken one each
     p.items = (packed ? cols / p.tile + n_seq : (cols + p.tile - 1) / p.tile * n_seq) * H;
