@@ -327,6 +327,12 @@ __device__ __forceinline__ int piece_swap(int row) {
 __device__ __forceinline__ s16x4_t read_transposed(const unsigned char* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)p);
 }
+// 16 bytes a lane from `offset` into LDS, behind one another from `to` on (uniform).  (The host's compiler does not know the size.)
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rows, unsigned char* to, int offset) {
+#ifdef __HIP_DEVICE_COMPILE__
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (__attribute__((address_space(3))) void*)to, 16, offset, 0, 0, 0);
+#endif
+}
 // rows of a sequence from `row` on, readable up to its last (zeros behind it)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const bf16_bits* first, int64_t stride, int row, int n, int D) {
     const int left = n - row;
@@ -340,7 +346,8 @@ template <int D, int NW>
 __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(PrefillArgs a) {
     constexpr int kThreads = 64 * NW, kCols = 32 * NW, kRowBytes = D * 2, kPieces = D / 8, kTileBytes = kTileKeys * kRowBytes;
     constexpr int kMine = kTileKeys * kPieces / kThreads, kSteps = D / 16, kBlocks = D / 32;
-    __shared__ __align__(16) unsigned char lds[2][2][kTileBytes];        // [buffer][keys, values]
+    // two buffers each, by names of their own: the compiler waits for loads that are on their way to a buffer before reads of that one only
+    __shared__ __align__(16) unsigned char keys0[kTileBytes], keys1[kTileBytes], values0[kTileBytes], values1[kTileBytes];
     __shared__ int not_finite[2];                                         // tile (from one) in the buffer whose values are not all finite
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, c = lane & 31;
     const int G = a.G;
@@ -362,41 +369,37 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) q[i] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(Q + 16 * i + 8 * half));
 
-    // staging: pieces of 16 bytes, consecutive threads along a row
-    u32x4_t kp[kMine], vp[kMine];
-    int put[kMine], k_off[kMine], v_off[kMine];
+    // staging: pieces of 16 bytes straight into LDS, 64 behind one another by a wave's instruction; which piece of a row goes where is
+    // decided by what each lane fetches
+    int k_off[kMine], v_off[kMine];
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-        const int p = tid + i * kThreads, row = p / kPieces, piece = p % kPieces;
-        put[i] = row * kRowBytes + (piece ^ piece_swap<D>(row)) * 16;
+        const int p = tid + i * kThreads, row = p / kPieces, piece = (p % kPieces) ^ piece_swap<D>(row);
         k_off[i] = row * (int)a.k.sr * 2 + piece * 16;
         v_off[i] = row * (int)a.v.sr * 2 + piece * 16;
     }
-    auto fetch_keys = [&](int tile) __attribute__((always_inline)) {
+    auto stage_keys = [&](int buf, int tile) __attribute__((always_inline)) {
         const auto rows = rows_from(K, a.k.sr, tile * kTileKeys, nk, D);
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) kp[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, k_off[i], 0, 0));
-    };
-    auto fetch_values = [&](int tile) __attribute__((always_inline)) {
-        const auto rows = rows_from(V, a.v.sr, tile * kTileKeys, nk, D);
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) vp[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, v_off[i], 0, 0));
-    };
-    auto stage_keys = [&](int buf) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) *reinterpret_cast<u32x4_t*>(&lds[buf][0][put[i]]) = kp[i];
+        for (int i = 0; i < kMine; ++i)
+            load_to_lds(rows, &(buf ? keys1 : keys0)[(i * kThreads + wave * 64) * 16], k_off[i]);
     };
     auto stage_values = [&](int buf, int tile) __attribute__((always_inline)) {
+        const auto rows = rows_from(V, a.v.sr, tile * kTileKeys, nk, D);
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) *reinterpret_cast<u32x4_t*>(&lds[buf][1][put[i]]) = vp[i];
-        if (tile >= n_whole) {                                            // only tiles that some column does not see all of ask for it
-            bool bad = false;
+        for (int i = 0; i < kMine; ++i)
+            load_to_lds(rows, &(buf ? values1 : values0)[(i * kThreads + wave * 64) * 16], v_off[i]);
+    };
+    // whether a tile's values are all finite: asked where some column does not see all of it
+    auto check_values = [&](int buf, int tile) __attribute__((always_inline)) {
+        bool bad = false;
 #pragma unroll
-            for (int i = 0; i < kMine; ++i)
+        for (int i = 0; i < kMine; ++i) {
+            const u32x4_t v = *reinterpret_cast<const u32x4_t*>(&(buf ? values1 : values0)[(i * kThreads + tid) * 16]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) bad |= (vp[i][e] & 0x7f80u) == 0x7f80u || (vp[i][e] & 0x7f800000u) == 0x7f800000u;
-            if (bad) not_finite[buf] = tile + 1;
+            for (int e = 0; e < 4; ++e) bad |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
         }
+        if (bad) not_finite[buf] = tile + 1;
     };
 
     f32x16_t o[kBlocks], z[2];                                            // output; logits of two blocks of 32 keys
@@ -407,7 +410,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(
     const int k_row = c * kRowBytes, k_swap = piece_swap<D>(c);
     const int i16 = lane & 15, v_row = 4 * half + (i16 >> 2);
     auto key_operand = [&](int buf, int b, int i) __attribute__((always_inline)) {
-        const unsigned char* at = lds[buf][0] + 32 * b * kRowBytes + k_row + (((2 * i + half) ^ k_swap) << 4);
+        const unsigned char* at = (buf ? keys1 : keys0) + 32 * b * kRowBytes + k_row + (((2 * i + half) ^ k_swap) << 4);
         return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(at));
     };
     auto value_operand = [&](int buf, int st, int b) __attribute__((always_inline)) {                    // keys 16 st ... of the tile, features of block b
@@ -415,7 +418,7 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int piece = 4 * b + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1), row = v_row + 8 * x;
-            v[x] = read_transposed(lds[buf][1] + (16 * st + row) * kRowBytes + (piece ^ piece_swap<D>(row)) * 16 + (i16 & 1) * 8);
+            v[x] = read_transposed((buf ? values1 : values0) + (16 * st + row) * kRowBytes + (piece ^ piece_swap<D>(row)) * 16 + (i16 & 1) * 8);
         }
         return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
@@ -497,15 +500,21 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(
     // first, the logits of the next tile's two.  A unit's logits are made beside the weights of the one before and its maximum
     // beside the outputs of that one, so that the matrix cores and the vector unit have independent work.  All reads of a
     // tile's keys, and of its values, lie between two barriers: keys one tile ahead of the values.
+    auto arrived = [&]() __attribute__((always_inline)) {                 // what all waves have asked for is in LDS
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
     bf16x8_t p[2];
     auto turn = [&](auto BUF, auto MASKED, int tile) __attribute__((always_inline)) {
         constexpr int buf = decltype(BUF)::value;
         constexpr bool masked = decltype(MASKED)::value;
-        __syncthreads();
-        stage_keys(buf);                                                  // tile + 2
-        fetch_keys(tile + 3);
+        arrived();
+        stage_keys(buf, tile + 2);
         stage_values(buf ^ 1, tile + 1);
-        fetch_values(tile + 2);
+        if constexpr (masked) {
+            check_values(buf, tile);
+            __syncthreads();
+        }
         const int k0 = tile * kTileKeys;
         if (masked && k0 >= wave_end) return;
         const bool odd_values = masked && not_finite[buf] == tile + 1;
@@ -528,15 +537,10 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(
         using I1 = std::integral_constant<int, 1>;
         if (tid < 2) not_finite[tid] = 0;
         __syncthreads();
-        fetch_keys(0);
-        fetch_values(0);
-        stage_keys(0);
+        stage_keys(0, 0);
         stage_values(0, 0);
-        fetch_keys(1);
-        fetch_values(1);
-        stage_keys(1);
-        fetch_keys(2);
-        __syncthreads();
+        stage_keys(1, 1);
+        arrived();
         logits(0, 0, z[0]);
         mask(z[0], 0);
         follow(z[0]);
