@@ -704,7 +704,7 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
             const float f = c.cum[at[i]];
             key[i] = c.idx[at[i]] <= newest ? weight_key(f) : kStays;
             key[i] = there ? key[i] : kStays;
-            may += __popcll(__ballot(key[i] != kStays));
+            may += __builtin_popcountll(__ballot(key[i] != kStays));
         }
         drop = lacking != 0 ? 0 : min(over, may);
         uint32_t leaves = 0;                                              // bit i: row 64 i + lane
@@ -731,8 +731,8 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
                 for (int i = 0; i < R; ++i) {
                     const bool tied = key[i] == cut.key, same = tied && place[i] == last.key;
                     const unsigned long long m = __ballot(same);
-                    if ((tied && place[i] < last.key) || (same && __popcll(m & ((1ull << lane) - 1)) < last.left)) leaves |= 1u << i;
-                    if (last.left != kAll) last.left -= __popcll(m);
+                    if ((tied && place[i] < last.key) || (same && __builtin_popcountll(m & ((1ull << lane) - 1)) < last.left)) leaves |= 1u << i;
+                    if (last.left != kAll) last.left -= __builtin_popcountll(m);          // below zero from here on (signed, as the builtin's counts are)
                 }
             }
         }
@@ -743,10 +743,10 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
             const int r = 64 * i + lane;
             const bool out = leaves >> i & 1, gap = out && r < stay, mover = !out && r >= stay && r < n;
             const unsigned long long g = __ballot(gap), m = __ballot(mover), lower = (1ull << lane) - 1;
-            if (gap) pairs[gaps + __popcll(g & lower)].x = at[i];
-            if (mover) pairs[movers + __popcll(m & lower)].y = at[i];
-            gaps += __popcll(g);
-            movers += __popcll(m);
+            if (gap) pairs[gaps + __builtin_popcountll(g & lower)].x = at[i];
+            if (mover) pairs[movers + __builtin_popcountll(m & lower)].y = at[i];
+            gaps += __builtin_popcountll(g);
+            movers += __builtin_popcountll(m);
         }
         if (lane == 0 && drop > 0) c.len[h] = stay;
     }

@@ -270,6 +270,22 @@ def _check_evict(ctx, c, budget, pos, w):
             assert np.array_equal(raw_bits(a), raw_bits(b[order])), h
 
 
+@pytest.mark.parametrize("lens", [[1016, 200, 65, 700], [1016, 200, 1400, 1500], [2600, 700, 129, 2000]])
+def test_evict_of_rows_that_are_all_alike(ctx, lens):
+    """One score and one position for hundreds of rows, more than a lane's or a thread's: the first rows leave, down to the budget exactly."""
+    page = 32
+    c, _ = _cache(ctx, lens, page, -(-(max(lens) + 1) // page), 64, torch.bfloat16, 41)
+    c.cum.fill_(0.5), c.idx.fill_(77)
+    _check_evict(ctx, c, [n // 2 for n in lens], [100] * 4, 4)
+    _check_evict(ctx, c, [n // 2 - 1 for n in lens], [100] * 4, 4)
+    for h, n in enumerate(lens):                                         # a third of the rows at one position more, some of more weight
+        rows = torch.arange(n // 2 - 1, device=DEV)
+        at = c.table[h, rows // page].long(), rows % page
+        c.idx[at] = torch.where(rows % 3 == 0, 78, 77).int()
+        c.cum[at] = torch.where(rows % 7 == 0, 0.75, 0.5)
+    _check_evict(ctx, c, [n // 4 for n in lens], [100] * 4, 4)
+
+
 @pytest.mark.parametrize("dtype,D,page", [(torch.bfloat16, 128, 64), (torch.float32, 128, 16), (torch.bfloat16, 64, 32), (torch.float32, 64, 256)])
 def test_evict_keeps_the_rows_of_most_weight(ctx, dtype, D, page):
     lens = [0, 1, 5, 64, 100, 300, 1000, 1023, 1024, 1500, 700]
