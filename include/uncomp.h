@@ -438,7 +438,9 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
  * belongs to one head and stands in its table once.  A table entry outside [0, n_pages) is no page;
  * rows there are not attended to and not written.  page is 16, 32, 64, 128 or 256;
  * max_pages*page <= 2^26; n_pages*page < 2^31; D 64 or 128; K_pages and V_pages 16-byte aligned.
- * Workspace of the three calls: uncomp_paged_workspace_bytes, rows = max_pages*page.
+ * Workspace of the three calls: uncomp_paged_workspace_bytes, rows = max_pages*page; where all tables
+ * together have room for more than twice the rows of the pool it goes by the pool, and that much is
+ * not needed (the message of UNCOMP_ERR_WORKSPACE says how much is).
  */
 typedef struct {
     void* K_pages;            /* [n_pages][page][D] of dtype                      */

@@ -34,7 +34,7 @@ bool strides_ok(const int64_t s[3], int D) {
     return s[0] >= 0 && s[1] >= 0 && s[2] >= D && (s[0] & 7) == 0 && (s[1] & 7) == 0 && (s[2] & 7) == 0;
 }
 
-constexpr int64_t kMostColumns = 1 << 30;
+constexpr int64_t kMostColumns = 1 << 30, kNoPool = INT64_MAX / 4;
 
 // The workspace starts at offset 0: scores' key ranges are overwritten, side-stream work of an earlier call may still use it.
 uncomp_status take_workspace(uncomp_ctx* ctx, const char* who, size_t need, void* stream) {
@@ -93,7 +93,7 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: sizes must be positive", who);
     if (!known_dtype(dtype)) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: dtype", who);
     if (D != 64 && D != 128) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: D must be 64 or 128", who);
-    if ((int64_t)q_rows * G > kMostColumns || k_rows > kMostColumns || n_seq > 1 << 20 || H > 1 << 20)
+    if ((int64_t)q_rows * G > kMostColumns || k_rows > kMostColumns || n_seq > 1 << 16 || H > 1 << 20)
         return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
     if (!strides_ok(q_strides, D) || !strides_ok(k_strides, D) || !strides_ok(v_strides, D) || !strides_ok(out_strides, D))
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: strides must be multiples of 8 elements, none negative, row strides >= D", who);
@@ -134,7 +134,7 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
 size_t uncomp_paged_workspace_bytes(int n_heads, int G, int D, int rows) {
     if (n_heads <= 0 || G <= 0 || D <= 0 || rows <= 0) return 0;
     size_t need = paged_append_bytes(n_heads);
-    const size_t step = plan_paged_step(n_heads, G, D, rows).bytes, evict = plan_paged_evict(n_heads, rows).bytes;
+    const size_t step = plan_paged_step(n_heads, G, D, rows, kNoPool).bytes, evict = plan_paged_evict(n_heads, rows, kNoPool).bytes;
     need = need > step ? need : step;
     return need > evict ? need : evict;
 }
@@ -178,8 +178,7 @@ uncomp_status uncomp_paged_step(uncomp_ctx* ctx, const uncomp_paged_cache* cache
     if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned4(pos) || !aligned4(out))
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: 16-byte aligned q, k_new and v_new required", who);
     const int rows = c.max_pages << c.shift;
-    if ((int64_t)c.n_heads * (rows / 256 + 64) > 0x7fffffffLL) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
-    const PagedStepPlan p = plan_paged_step(c.n_heads, G, cache->D, rows);
+    const PagedStepPlan p = plan_paged_step(c.n_heads, G, cache->D, rows, (int64_t)c.n_pages << c.shift);
     st = take_workspace(ctx, who, p.bytes, stream);
     if (st != UNCOMP_OK) return st;
     OnDevice on(ctx->device);
@@ -200,7 +199,7 @@ uncomp_status uncomp_paged_evict(uncomp_ctx* ctx, const uncomp_paged_cache* cach
     if (budget == nullptr || pos == nullptr) return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: null pointer", who);
     if (w < 0) return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: w must not be negative", who);
     if (!aligned4(budget) || !aligned4(pos) || !aligned4(evicted)) return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: misaligned pointer", who);
-    const PagedEvictPlan p = plan_paged_evict(c.n_heads, c.max_pages << c.shift);
+    const PagedEvictPlan p = plan_paged_evict(c.n_heads, c.max_pages << c.shift, (int64_t)c.n_pages << c.shift);
     st = take_workspace(ctx, who, p.bytes, stream);
     if (st != UNCOMP_OK) return st;
     OnDevice on(ctx->device);

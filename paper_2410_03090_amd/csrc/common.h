@@ -270,26 +270,31 @@ struct PagedCache {
     int32_t* len;
     int n_heads, n_pages, shift, max_pages;
 };
+// Arrays in the workspace with an entry for every row of every head have as many as the tables have room for, head behind head; or, where
+// that is more than twice the rows of the pool (by_pool), one for each of those.  By the tables / by the pool, us: steps of 8 heads of 128K rows
+// 127 / 131, of 256 heads of 16K 479 / 481; a half of them evicted 242 / 291 and 86 / 99.
 struct PagedStepPlan {
     bool one_launch;     // a workgroup per head, nothing in the workspace
     int n_split;         // parts of all heads together, but for one broken one of each
     int rows;            // rows a head's table has room for
+    bool by_pool;
     size_t head_off;     // int4  [n_heads]: rows before and after, first part, parts
     size_t ml_off;       // float2 [n_split + n_heads][G]
     size_t acc_off;      // float [n_split + n_heads][G][D]
-    size_t logit_off;    // float [n_heads][query heads, rounded up to 4, 8 or 16][rows]
+    size_t logit_off;    // float [n_heads][query heads, rounded up to 4, 8 or 16][rows], or [n_pages][query heads, as much][page]
     size_t bytes;
 };
-PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows);
+PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows, int64_t pool_rows);
 struct PagedEvictPlan {
-    int pairs;           // most rows of one head that move
+    int rows;
+    bool by_pool;
     size_t count_off;    // int32 [n_heads]
-    size_t pair_off;     // int2  [n_heads][pairs]: to, from (rows of the pool)
-    int key_rows;        // tables whose keys do not fit in LDS: rows a head has in
-    size_t key_off;      // uint32 [n_heads][key_rows]
+    size_t pair_off;     // int2  [entries]: to, from (rows of the pool); a head's i-th at the entry of its row i
+    bool keys_in_lds;
+    size_t key_off;      // uint32 [entries], where they are not
     size_t bytes;
 };
-PagedEvictPlan plan_paged_evict(int n_heads, int rows);
+PagedEvictPlan plan_paged_evict(int n_heads, int rows, int64_t pool_rows);
 size_t paged_append_bytes(int n_heads);
 hipError_t launch_paged_append(const PagedCache& c, const void* K, const void* V, const int32_t* idx, const float* cum, const int32_t* rows_in,
                                int rows, int64_t head_bytes, int64_t row_bytes, int row_size, char* ws, const Env& env);

@@ -12,13 +12,13 @@ namespace uncomp {
 namespace {
 
 constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / 64;
-constexpr int kFinishThreads = 256, kFinishRows = 1024;
+constexpr int kFinishThreads = 256, kFinishRows = 1024, kFinishWgs = 8192;      // kFinishWgs: about the most workgroups for rows, whatever room the tables have
 constexpr int kSplitAim = 768;                        // workgroups of the attention of few heads: three a CU
 constexpr int kLeastShare = 128;                      // rows of a workgroup, at least: a block a wave
 // One workgroup a head: from as many heads on as fill the chip, with logits that leave room for two workgroups on a CU.
 constexpr int kHeadLaunchHeads = 512;
 constexpr size_t kHeadLaunchLds = 76 * 1024;
-constexpr int kSelectThreads = 1024, kSelectKeys = 32768, kWaveSelectHeads = 512;      // threads of a selection, keys that it holds in LDS
+constexpr int kSelectThreads = 1024, kSelectKeys = 32768, kWaveSelectHeads = 512, kWaveSelectRows = 32;      // threads of a selection, keys that it holds in LDS; a wave's most rows a lane
 
 __device__ __forceinline__ int head_rows(const PagedCache& c, int h) {
     const int cap = c.max_pages << c.shift;
@@ -30,6 +30,12 @@ __device__ __forceinline__ bool page_ok(const PagedCache& c, int id) { return (u
 __device__ __forceinline__ int64_t pool_row(const PagedCache& c, int h, int r) {
     const int id = c.table[(int64_t)h * c.max_pages + (r >> c.shift)];
     return page_ok(c, id) ? ((int64_t)id << c.shift) + (r & ((1 << c.shift) - 1)) : -1;
+}
+
+// entry of row r of head h in the workspace's arrays (of a head with all its pages)
+template <bool POOL>
+__device__ __forceinline__ int64_t row_entry(const PagedCache& c, int h, int r) {
+    return POOL ? pool_row(c, h, r) : (int64_t)h * (c.max_pages << c.shift) + r;
 }
 
 template <int BYTES>
@@ -380,7 +386,7 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_attend_kernel(PagedCa
     const int size = (hr.n / hp.n_parts + A::kBlock) / A::kBlock * A::kBlock;                 // whole blocks, together more than n rows
     const int begin = hp.part * size, end = begin + size, blocks = hr.n / A::kBlock;
     const bool tail = hr.n1 > blocks * A::kBlock && blocks * A::kBlock >= begin && blocks * A::kBlock < end;
-    float* logits = reinterpret_cast<float*>(ws + p.logit_off) + (int64_t)h * GT * p.rows;
+    float* logits = reinterpret_cast<float*>(ws + p.logit_off) + (p.by_pool ? 0 : (int64_t)h * GT * p.rows);
     attend_rows<T, D>(a, c, h, hr, k_new + (int64_t)h * D, v_new + (int64_t)h * D, begin + A::kBlock * wave, kStep, min(end, blocks * A::kBlock),
                       tail && (blocks - begin / A::kBlock) % kAttendWaves == wave, lane, [&](int r, const float (&s)[A::kPerLane]) {
         // a wave's logits change places in LDS (in the order its instructions have there) for stores of whole pieces of 16 bytes
@@ -394,7 +400,15 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_attend_kernel(PagedCa
 #pragma unroll
         for (int i = 0; i < (GT * A::kBlock + 255) / 256; ++i) {
             const int x = 4 * (lane + 64 * i), g = x / A::kBlock, in = x % A::kBlock;
-            if (g < GT) *reinterpret_cast<f32x4_t*>(logits + (int64_t)g * p.rows + r + in) = *reinterpret_cast<const f32x4_t*>(mine + g * kLine + in);
+            if (g >= GT) continue;
+            int64_t to = (int64_t)g * p.rows + r + in;
+            if (p.by_pool) {
+                const int page = (r + in) >> c.shift;                        // (a block may reach behind the table)
+                const int id = page < c.max_pages ? c.table[(int64_t)h * c.max_pages + page] : -1;
+                if (!page_ok(c, id)) continue;
+                to = (((int64_t)id * GT + g) << c.shift) + ((r + in) & ((1 << c.shift) - 1));
+            }
+            *reinterpret_cast<f32x4_t*>(logits + to) = *reinterpret_cast<const f32x4_t*>(mine + g * kLine + in);
         }
         __builtin_amdgcn_wave_barrier();
     });
@@ -435,9 +449,9 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_attend_kernel(PagedCa
     if (hp.part == 0 && threadIdx.x == 0) reinterpret_cast<int4*>(ws + p.head_off)[h] = make_int4(hr.n, hr.n1, blockIdx.x, hp.n_parts);
 }
 
-// Joins the parts.  The first n_chunks workgroups of a head take 1024 rows each and add their weights to cum; the rest take a share of the
-// outputs, several threads to four features of them; the first also writes the new row.
-template <typename T, int D, int GT>
+// Joins the parts.  The first n_chunks workgroups of a head take 1024 rows at a time and add their weights to cum; the rest take a share
+// of the outputs, several threads to four features of them; the first also writes the new row.
+template <typename T, int D, int GT, bool POOL>
 __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache c, const T* __restrict__ k_new, const T* __restrict__ v_new,
                                                                       const int32_t* __restrict__ pos, int G, int n_chunks, int n_join,
                                                                       PagedStepPlan p, const char* __restrict__ ws, float* __restrict__ out) {
@@ -454,13 +468,20 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache
     constexpr int kRows = kFinishRows / kFinishThreads;
     RowPlaces<kRows> places;
     RowLogits<GT> row[kRows];
-    if (rows) {
-        const int first = task * kFinishRows + threadIdx.x;
-        const float* logits = reinterpret_cast<const float*>(ws + p.logit_off) + (int64_t)h * GT * p.rows;
+    const float* logits = reinterpret_cast<const float*>(ws + p.logit_off) + (POOL ? 0 : (int64_t)h * GT * p.rows);
+    const auto fetch = [&](int first) __attribute__((always_inline)) {
+        if (!POOL)
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) row[i].load(logits + min(first + i * kFinishThreads, p.rows - 1), p.rows);
+            for (int i = 0; i < kRows; ++i) row[i].load(logits + min(first + i * kFinishThreads, p.rows - 1), p.rows);
         places.fetch(c, h, first, kFinishThreads, n, n1);
-    }
+        if (POOL)
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int64_t at = places.at[i] < 0 ? 0 : places.at[i], mask = (1 << c.shift) - 1;
+                row[i].load(logits + (at & ~mask) * GT + (at & mask), mask + 1);
+            }
+    };
+    if (rows) fetch(task * kFinishRows + threadIdx.x);
     // maximum and sum of every query head, a wave each
     if (threadIdx.x < 16) norm[threadIdx.x] = make_float2(0.f, 0.f);
     __syncthreads();
@@ -475,9 +496,14 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache
     }
     __syncthreads();
     if (rows) {
+        for (int first = task * kFinishRows;;) {
 #pragma unroll
-        for (int i = 0; i < kRows; ++i)
-            if (places.at[i] >= 0) c.cum[places.at[i]] = places.cum[i] + row[i].weight(norm);
+            for (int i = 0; i < kRows; ++i)
+                if (places.at[i] >= 0) c.cum[places.at[i]] = places.cum[i] + row[i].weight(norm);
+            first += n_chunks * kFinishRows;
+            if (first >= n1) break;
+            fetch(first + threadIdx.x);
+        }
         if (task == 0 && n1 > n) write_new_row<T, D>(c, h, n, k_new + (int64_t)h * D, v_new + (int64_t)h * D, pos, kFinishThreads);
         return;
     }
@@ -681,7 +707,7 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
     if (wg >= c.n_heads) return;
     const int h = spread_head(wg, c.n_heads), n = head_rows(c, h), over = rows_over(n, budget[h], w);
     const int64_t newest = (int64_t)pos[h] - w;
-    int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off) + (int64_t)h * p.pairs;
+    int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off) + (int64_t)h * p.rows;          // (never by the pool)
     const int32_t* table = c.table + (int64_t)h * c.max_pages;
     const int in_page = (1 << c.shift) - 1;
     int drop = 0, gaps = 0;
@@ -756,22 +782,25 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
     }
 }
 
-// Keys of tables that do not fit in LDS, made by as many workgroups as there are: 1024 rows each.
+// Keys of tables that do not fit in LDS, 1024 rows of a head at a time.
 __global__ __launch_bounds__(256) void paged_key_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos, int w,
                                                         PagedEvictPlan p, int n_chunks, char* ws) {
     const int h = blockIdx.x / n_chunks, n = head_rows(c, h);
     if (rows_over(n, budget[h], w) == 0) return;
     const int64_t newest = (int64_t)pos[h] - w;
-    uint32_t* key = reinterpret_cast<uint32_t*>(ws + p.key_off) + (int64_t)h * p.key_rows;
-    const int first = blockIdx.x % n_chunks * 1024 + threadIdx.x;
+    uint32_t* key = reinterpret_cast<uint32_t*>(ws + p.key_off);
+    for (int first = blockIdx.x % n_chunks * 1024 + threadIdx.x; first < n; first += n_chunks * 1024)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = first + 256 * i;
-        if (r < n) key[r] = row_key(c, pool_row(c, h, r), newest);
-    }
+        for (int i = 0; i < 4; ++i) {
+            const int r = first + 256 * i;
+            if (r >= n) continue;
+            const int64_t at = pool_row(c, h, r), to = p.by_pool ? at : (int64_t)h * p.rows + r;
+            if (to >= 0) key[to] = row_key(c, at, newest);
+        }
 }
 
 // Longer tables: a workgroup per head, keys in LDS where they fit and from the workspace otherwise, four at a time.
+template <bool POOL>
 __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos,
                                                                       int w, PagedEvictPlan p, char* ws, int32_t* __restrict__ evicted) {
     extern __shared__ __align__(16) uint32_t key_s[];
@@ -782,15 +811,20 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache
     const int h = spread_head(blockIdx.x, gridDim.x), tid = threadIdx.x;
     const int n = head_rows(c, h), over = rows_over(n, budget[h], w);
     const int64_t newest = (int64_t)pos[h] - w;
-    int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off) + (int64_t)h * p.pairs;
-    const bool in_lds = p.key_rows == 0;
-    const uint32_t* key_m = reinterpret_cast<const uint32_t*>(ws + p.key_off) + (int64_t)h * p.key_rows;
+    int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off);
+    const bool in_lds = p.keys_in_lds;
+    const uint32_t* key_m = reinterpret_cast<const uint32_t*>(ws + p.key_off) + (POOL ? 0 : (int64_t)h * p.rows);
     if (in_lds && over > 0) {
 #pragma unroll 4
         for (int r = tid; r < n; r += kSelectThreads) key_s[r] = row_key(c, pool_row(c, h, r), newest);
         __syncthreads();
     }
-    const auto four = [&](int r) { return in_lds ? *reinterpret_cast<const uint4*>(key_s + r) : *reinterpret_cast<const uint4*>(key_m + r); };
+    const auto four = [&](int r) __attribute__((always_inline)) {
+        if (in_lds) return *reinterpret_cast<const uint4*>(key_s + r);
+        if (!POOL) return *reinterpret_cast<const uint4*>(key_m + r);
+        const int64_t at = pool_row(c, h, r);
+        return at < 0 ? make_uint4(kLacks, kLacks, kLacks, kLacks) : *reinterpret_cast<const uint4*>(key_m + at);
+    };
     // f(row, key) of every row from `begin` to `end`, `step` rows between fours
     const auto each_key = [&](int begin, int end, int step, auto&& f) __attribute__((always_inline)) {
         for (int r = begin; r < end; r += step) {
@@ -859,13 +893,15 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache
         c.len[h] = stay;
     }
     int from = block_scan(movers, buf, &total);
-    each_row([&](int r) { pairs[to++].x = (int)pool_row(c, h, r); }, [&](int r) { pairs[from++].y = (int)pool_row(c, h, r); });
+    each_row([&](int r) { pairs[row_entry<POOL>(c, h, to++)].x = (int)pool_row(c, h, r); },
+             [&](int r) { pairs[row_entry<POOL>(c, h, from++)].y = (int)pool_row(c, h, r); });
 }
 
 // Moves the paired rows: 16 bytes a lane of K and of V, four pairs at a time.
+template <bool POOL>
 __global__ __launch_bounds__(256) void paged_move_kernel(PagedCache c, int row_size, int n_chunks, PagedEvictPlan p, const char* __restrict__ ws) {
     const int h = spread_head(blockIdx.x / n_chunks, c.n_heads);
-    const int2* pairs = reinterpret_cast<const int2*>(ws + p.pair_off) + (int64_t)h * p.pairs;
+    const int2* pairs = reinterpret_cast<const int2*>(ws + p.pair_off);
     const int n = reinterpret_cast<const int32_t*>(ws + p.count_off)[h];
     const int lanes = row_size / 16, per = 256 / lanes, piece = (threadIdx.x % lanes) * 16;
     char* K = static_cast<char*>(c.K);
@@ -878,7 +914,7 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedCache c, int row_s
         int32_t idx[kAhead];
         float cum[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) m[i] = pairs[min(i0 + i * step, n - 1)];
+        for (int i = 0; i < kAhead; ++i) m[i] = pairs[row_entry<POOL>(c, h, min(i0 + i * step, n - 1))];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const int64_t from = m[i].y;
@@ -911,7 +947,7 @@ size_t head_step_lds(int G, int D, int rows) {
 }
 }  // namespace
 
-PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows) {
+PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows, int64_t pool_rows) {
     PagedStepPlan p{};
     p.rows = (rows + 31) / 32 * 32;                                       // whole blocks are written
     p.one_launch = n_heads >= kHeadLaunchHeads && head_step_lds(G, D, p.rows) <= kHeadLaunchLds;
@@ -927,22 +963,31 @@ PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows) {
         off = align_up(off + bytes, 256);
         return at;
     };
+    p.by_pool = 2 * pool_rows < (int64_t)n_heads * p.rows;
     p.head_off = take((size_t)n_heads * sizeof(int4));
     p.ml_off = take(parts * G * sizeof(float2));
     p.acc_off = take(parts * G * D * sizeof(float));
-    p.logit_off = take((size_t)n_heads * p.rows * heads_bound(G) * sizeof(float));
+    p.logit_off = take((size_t)(p.by_pool ? pool_rows : (int64_t)n_heads * p.rows) * heads_bound(G) * sizeof(float));
     p.bytes = off;
     return p;
 }
 
-PagedEvictPlan plan_paged_evict(int n_heads, int rows) {
+PagedEvictPlan plan_paged_evict(int n_heads, int rows, int64_t pool_rows) {
     PagedEvictPlan p{};
-    p.pairs = rows / 2 + 1;
-    p.key_rows = rows > kSelectKeys ? (rows + 3) & ~3 : 0;
-    p.count_off = 0;
-    p.pair_off = align_up((size_t)n_heads * sizeof(int32_t), 256);
-    p.key_off = align_up(p.pair_off + (size_t)n_heads * p.pairs * sizeof(int2), 256);
-    p.bytes = p.key_off + (size_t)n_heads * p.key_rows * sizeof(uint32_t);
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = align_up(off + bytes, 256);
+        return at;
+    };
+    p.rows = rows;
+    p.by_pool = rows > 64 * kWaveSelectRows && 2 * pool_rows < (int64_t)n_heads * rows;
+    const size_t entries = p.by_pool ? pool_rows : (int64_t)n_heads * rows;
+    p.keys_in_lds = rows <= kSelectKeys;
+    p.count_off = take((size_t)n_heads * sizeof(int32_t));
+    p.pair_off = take(entries * sizeof(int2));
+    p.key_off = take(p.keys_in_lds ? 0 : entries * sizeof(uint32_t));
+    p.bytes = off;
     return p;
 }
 
@@ -980,13 +1025,14 @@ hipError_t step_of(const PagedCache& c, const void* q, const void* k_new, const 
         c, static_cast<const T*>(q), kn, vn, G, p, ws);
     env.end();
     // a workgroup joins up to 64 KiB of partial outputs, of at most as many quads as it has threads
-    const int n_chunks = (p.rows + kFinishRows - 1) / kFinishRows;
+    const int n_chunks = min((p.rows + kFinishRows - 1) / kFinishRows, kFinishWgs / c.n_heads + 1);
     const int n_parts = (p.n_split + c.n_heads - 1) / c.n_heads;
     int n_join = (int)(((int64_t)n_parts * G * D * 4 + 65535) / 65536);
     const int least = (G * D / 4 + kFinishThreads - 1) / kFinishThreads;
     n_join = out == nullptr ? 0 : n_join < least ? least : n_join;
     env.begin("paged_finish");
-    paged_finish_kernel<T, D, GT><<<c.n_heads * (n_chunks + n_join), kFinishThreads, 0, env.s>>>(c, kn, vn, pos, G, n_chunks, n_join, p, ws, out);
+    const auto finish = p.by_pool ? paged_finish_kernel<T, D, GT, true> : paged_finish_kernel<T, D, GT, false>;
+    finish<<<c.n_heads * (n_chunks + n_join), kFinishThreads, 0, env.s>>>(c, kn, vn, pos, G, n_chunks, n_join, p, ws, out);
     env.end();
     return hipGetLastError();
 }
@@ -1014,7 +1060,8 @@ hipError_t init_paged_kernels() {
                 });
                 if (e != hipSuccess) return e;
             }
-    return allow_dynamic_lds(reinterpret_cast<const void*>(paged_select_kernel), kSelectKeys * sizeof(uint32_t));
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(paged_select_kernel<false>), kSelectKeys * sizeof(uint32_t));
+    return e != hipSuccess ? e : allow_dynamic_lds(reinterpret_cast<const void*>(paged_select_kernel<true>), kSelectKeys * sizeof(uint32_t));
 }
 
 hipError_t launch_paged_step(const PagedCache& c, const void* q, const void* k_new, const void* v_new, uncomp_dtype dt, const int32_t* pos, int G,
@@ -1036,20 +1083,22 @@ hipError_t launch_paged_evict(const PagedCache& c, const int32_t* budget, const 
     if (rows <= 64 * 8) wave_form(std::integral_constant<int, 8>{});
     else if (rows <= 64 * 16) wave_form(std::integral_constant<int, 16>{});
     else if (rows <= 64 * 24 && rows <= least) wave_form(std::integral_constant<int, 24>{});
-    else if (rows <= 64 * 32 && rows <= least) wave_form(std::integral_constant<int, 32>{});
+    else if (rows <= 64 * kWaveSelectRows && rows <= least) wave_form(std::integral_constant<int, kWaveSelectRows>{});
     else {
-        if (p.key_rows > 0) {
-            const int n_chunks = (rows + 1023) / 1024;
+        if (!p.keys_in_lds) {
+            const int most = (rows + 1023) / 1024, n_chunks = min(most, (4096 + c.n_heads - 1) / c.n_heads);
             paged_key_kernel<<<c.n_heads * n_chunks, 256, 0, env.s>>>(c, budget, pos, w, p, n_chunks, ws);
         }
-        paged_select_kernel<<<c.n_heads, kSelectThreads, p.key_rows > 0 ? 0 : (size_t)(rows + 3) / 4 * 16, env.s>>>(c, budget, pos, w, p, ws, evicted);
+        const auto select = p.by_pool ? paged_select_kernel<true> : paged_select_kernel<false>;
+        select<<<c.n_heads, kSelectThreads, p.keys_in_lds ? (size_t)(rows + 3) / 4 * 16 : 0, env.s>>>(c, budget, pos, w, p, ws, evicted);
     }
     env.end();
     int n_chunks = 2048 / c.n_heads;
-    const int most = (p.pairs + 31) / 32;
+    const int most = (rows / 2 + 31) / 32;
     n_chunks = n_chunks < 1 ? 1 : (n_chunks > most ? most : n_chunks);
     env.begin("paged_move");
-    paged_move_kernel<<<c.n_heads * n_chunks, 256, 0, env.s>>>(c, row_size, n_chunks, p, ws);
+    const auto move = p.by_pool ? paged_move_kernel<true> : paged_move_kernel<false>;
+    move<<<c.n_heads * n_chunks, 256, 0, env.s>>>(c, row_size, n_chunks, p, ws);
     env.end();
     return hipGetLastError();
 }

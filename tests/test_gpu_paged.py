@@ -176,6 +176,41 @@ def test_queries_alone_missing_pages_and_lengths_out_of_range(ctx, dtype):
     assert np.array_equal(state[0][int(c.table[0, 5])], raw_bits(c.K[int(c.table[0, 5])]))
 
 
+@pytest.mark.parametrize("n,G,max_pages,mib", [(6, 4, 2500, 3), (100, 16, 600, 8), (700, 8, 2500, 24)])
+def test_tables_with_more_room_than_the_pool_has_rows(ctx, n, G, max_pages, mib):
+    """Tables for thousands of rows a head over a pool of a few pages each: the workspace goes by the pool.  Steps and evictions; a head that counts
+    rows without pages leaves the others alone."""
+    from paper_2410_03090_amd import binding
+    D, page, dtype = 64, 16, torch.bfloat16
+    g = torch.Generator().manual_seed(n)
+    lens = torch.randint(0, 90, (n,), generator=g).tolist()
+    lens[-1] = 300
+    c, _ = _cache(ctx, lens, page, max_pages, D, dtype, 40, room=2)
+    small = binding.Context(0, mib << 20)
+    assert binding.Context.paged_workspace_bytes(n, G, D, max_pages * page) > mib << 20
+    pick = [0, 1, 2, n // 2, n - 2, n - 1]
+    for t in range(2):
+        q, kn, vn = _token(n, G, D, dtype, 80 + t)
+        before = {h: _rows(c, h) for h in pick}
+        pos = torch.full((n,), 10 ** 6 + t, dtype=torch.int32, device=DEV)
+        out = small.paged_step(c, q.to(DEV), kn.to(DEV), vn.to(DEV), pos)
+        torch.cuda.synchronize()
+        for h in pick:
+            _check_step(before[h], _rows(c, h), q[h], kn[h], vn[h], 10 ** 6 + t, out[h].cpu(), dtype, f"token {t}, head {h}")
+    _check_evict(small, c, [max(5, m // 2) for m in lens], [10 ** 7] * n, 4)
+    c.length[0] = max_pages * page - 1000                                                  # rows that it has no pages for
+    before = {h: _rows(c, h) for h in pick[1:]}
+    q, kn, vn = _token(n, G, D, dtype, 90)
+    out = small.paged_step(c, q.to(DEV), kn.to(DEV), vn.to(DEV), torch.full((n,), 2 * 10 ** 6, dtype=torch.int32, device=DEV))
+    evicted = small.paged_evict(c, torch.zeros(n, dtype=torch.int32, device=DEV), torch.zeros(n, dtype=torch.int32, device=DEV), 10 ** 6)
+    torch.cuda.synchronize()
+    assert c.length[0] == max_pages * page - 1000 and (evicted == 0).all()
+    for h in pick[1:]:
+        after = _rows(c, h)
+        assert torch.equal(after[2][:-1], before[h][2]) and out[h].isfinite().all()
+    small.close()
+
+
 def test_infinite_values_and_logits(ctx):
     G, D, page = 2, 128, 32
     c, _ = _cache(ctx, [200, 200, 200], page, 7, D, torch.bfloat16, 13)
@@ -488,7 +523,7 @@ def test_refusals(ctx):
     for kw in (dict(c=None), dict(b=None), dict(pos=None), dict(w=-1), dict(b=p + 2)):
         assert evict(**kw) == binding.ERR_INVALID_ARG, kw
     small = binding.Context(0, 1 << 15)
-    big = cache(max_pages=1 << 16)
+    big = cache(max_pages=1 << 16, n_pages=1 << 20)
     assert lib.uncomp_paged_step(small.handle, big, p, 4, p, p, p, p, None) == binding.ERR_WORKSPACE
     assert lib.uncomp_paged_evict(small.handle, big, p, p, 4, None, None) == binding.ERR_WORKSPACE
     assert b"workspace" in lib.uncomp_last_error(small.handle)
