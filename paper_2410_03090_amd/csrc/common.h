@@ -274,7 +274,9 @@ struct PagedCache {
 // that is more than twice the rows of the pool (by_pool), one for each of those.  By the tables / by the pool, us: steps of 8 heads of 128K rows
 // 127 / 131, of 256 heads of 16K 479 / 481; a half of them evicted 242 / 291 and 86 / 99.
 struct PagedStepPlan {
-    bool one_launch;     // a workgroup per head, nothing in the workspace
+    int head_rows;       // > 0: a workgroup for each head of fewer rows
+    bool split;          // the other heads in parts
+    size_t list_off;     // where there are such of both kinds: int64 rows of the others together and a token each, int32 their number, int32 [n_heads] they
     int n_split;         // parts of all heads together, but for one broken one of each
     int rows;            // rows a head's table has room for
     bool by_pool;

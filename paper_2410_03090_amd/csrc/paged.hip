@@ -15,9 +15,12 @@ constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / 64;
 constexpr int kFinishThreads = 256, kFinishRows = 1024, kFinishWgs = 8192;      // kFinishWgs: about the most workgroups for rows, whatever room the tables have
 constexpr int kSplitAim = 768;                        // workgroups of the attention of few heads: three a CU
 constexpr int kLeastShare = 128;                      // rows of a workgroup, at least: a block a wave
-// One workgroup a head: from as many heads on as fill the chip, with logits that leave room for two workgroups on a CU.
+// One workgroup a head: from as many heads on as fill the chip, with logits that leave room for two workgroups on a CU.  Where tables have room
+// for more rows than that, for the heads that hold few enough for three; the rest in parts.  All heads in parts / so, us, heads of G 4 with tables
+// for 8192 and 20480 rows: 600 of 350 - 700 rows 77 / 47, 5120 of them 674 / 326, 600 of 1500 - 3000 189 / 167, 600 of 3000 - 6000 (a few of
+// them short) 340 / 420, 600 of 10000 - 20000 1046 / 1062.
 constexpr int kHeadLaunchHeads = 512;
-constexpr size_t kHeadLaunchLds = 76 * 1024;
+constexpr size_t kHeadLaunchLds = 76 * 1024, kShortHeadLds = 50 * 1024;
 constexpr int kSelectThreads = 1024, kSelectKeys = 32768, kWaveSelectHeads = 512, kWaveSelectRows = 32;      // threads of a selection, keys that it holds in LDS; a wave's most rows a lane
 
 __device__ __forceinline__ int head_rows(const PagedCache& c, int h) {
@@ -251,16 +254,17 @@ struct RowLogits {
 }  // namespace
 
 // GT: bound on the query heads per KV head.
-// Many heads: one workgroup per head does all of the step.  The logits stay in LDS until the sums are known; then every row's weights go to
+// Many heads: one workgroup per head does all of the step (some: if it has fewer than `stride` rows).  The logits stay in LDS until the sums are known; then every row's weights go to
 // its cum, and the waves' outputs are joined in the same LDS.
 template <typename T, int D, int GT>
 __global__ __launch_bounds__(kAttendThreads, 3) void paged_head_kernel(PagedCache c, const T* __restrict__ q, const T* __restrict__ k_new,
                                                                     const T* __restrict__ v_new, const int32_t* __restrict__ pos, int G,
-                                                                    int stride, float* __restrict__ out) {
+                                                                    int stride, bool some, float* __restrict__ out) {
     using A = WaveAttend<T, D>;
     extern __shared__ float dyn[];                                        // logits [GT][stride], then outputs [waves][G][D]
     __shared__ float ml_s[kAttendWaves][16][2];
     const int h = spread_head(blockIdx.x, gridDim.x), lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, j = lane >> 4;
+    if (some && head_rows(c, h) >= stride) return;
     const T* kn = k_new + (int64_t)h * D;
     const T* vn = v_new + (int64_t)h * D;
     A a;
@@ -330,21 +334,70 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_head_kernel(PagedCach
     }
 }
 
-// Few heads: their rows are dealt to about as many workgroups as run at a time, whatever the heads' lengths: as many parts of a head as it has
-// shares of all rows, begun ones included, and all of one size.  Workgroup number -> head and part, from the lengths, 64 of them at a time.
+// The heads of at least `least` rows, in order, and their rows.  One workgroup, a run of heads a thread.  (Before any length changes.)
+__global__ __launch_bounds__(1024) void paged_list_kernel(PagedCache c, int least, PagedStepPlan p, char* ws) {
+    __shared__ int count_s[16];
+    __shared__ int64_t rows_s[16];
+    int64_t* total = reinterpret_cast<int64_t*>(ws + p.list_off);
+    int32_t* list = reinterpret_cast<int32_t*>(total + 1);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int run = (c.n_heads + 1023) / 1024, begin = min(c.n_heads, tid * run), end = min(c.n_heads, begin + run);
+    int mine = 0;
+    int64_t rows = 0;
+    for (int h = begin; h < end; ++h) {
+        const int n = head_rows(c, h);
+        mine += n >= least;
+        rows += n >= least ? n + 1 : 0;
+    }
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += u;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) rows += __shfl_xor(rows, o, 64);
+    if (lane == 63) count_s[wave] = sum;
+    if (lane == 63) rows_s[wave] = rows;
+    __syncthreads();
+    int at = sum - mine;
+    for (int x = 0; x < wave; ++x) at += count_s[x];
+    for (int h = begin; h < end; ++h)
+        if (head_rows(c, h) >= least) list[1 + at++] = h;
+    if (tid == 1023) {
+        list[0] = at;
+        int64_t t = 0;
+        for (int x = 0; x < 16; ++x) t += rows_s[x];
+        *total = t;
+    }
+}
+
+// The rows of few heads, or of the listed ones, are dealt to about as many workgroups as run at a time, whatever the heads' lengths: as many parts
+// of a head as it has shares of all rows, begun ones included, and all of one size.  Part number -> head and part of it, from the
+// lengths, 64 of them at a time.
 struct HeadPart {
     int h, part, n_parts;
 };
-__device__ __forceinline__ bool find_head_part(const PagedCache& c, const PagedStepPlan& p, int wg, HeadPart* out) {
+template <bool LISTED>
+__device__ __forceinline__ bool find_head_part(const PagedCache& c, const PagedStepPlan& p, const char* ws, int wg, HeadPart* out) {
     const int lane = threadIdx.x & 63;
+    const int64_t* listed = reinterpret_cast<const int64_t*>(ws + p.list_off);
+    const int32_t* list = reinterpret_cast<const int32_t*>(listed + 1);
+    const int n_heads = LISTED ? list[0] : c.n_heads;
     int64_t total = 0;
-    for (int h = lane; h < c.n_heads; h += 64) total += head_rows(c, h) + 1;
+    if (LISTED) {
+        if (wg >= p.n_split + n_heads) return false;
+        total = *listed;
+    } else {
+        for (int h = lane; h < c.n_heads; h += 64) total += head_rows(c, h) + 1;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+        for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+    }
     int share = max(kLeastShare, (int)((total + p.n_split - 1) / p.n_split));
     if (share < 4 * kLeastShare) share = (share + kLeastShare - 1) / kLeastShare * kLeastShare;      // as many blocks for every wave, where they are few
-    for (int h0 = 0; h0 < c.n_heads; h0 += 64) {
-        const int parts = h0 + lane < c.n_heads ? head_rows(c, h0 + lane) / share + 1 : 0;
+    for (int h0 = 0; h0 < n_heads; h0 += 64) {
+        const int i = min(h0 + lane, n_heads - 1), h = LISTED ? list[1 + i] : i;
+        const int parts = h0 + lane < n_heads ? head_rows(c, h) / share + 1 : 0;
         int sum = parts;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -354,7 +407,7 @@ __device__ __forceinline__ bool find_head_part(const PagedCache& c, const PagedS
         const unsigned long long has = __ballot(sum > wg);
         if (has != 0) {
             const int x = __builtin_amdgcn_readfirstlane(__ffsll(has) - 1);
-            out->h = h0 + x;
+            out->h = __builtin_amdgcn_readlane(h, x);
             out->n_parts = __builtin_amdgcn_readlane(parts, x);
             out->part = wg - (__builtin_amdgcn_readlane(sum, x) - out->n_parts);
             return true;
@@ -366,7 +419,7 @@ __device__ __forceinline__ bool find_head_part(const PagedCache& c, const PagedS
 
 // One part of one head's rows per workgroup, its blocks dealt to the waves in turn.  Leaves the part's maximum, sum and output
 // (joined by the finishing kernel) and every row's logits.
-template <typename T, int D, int GT>
+template <typename T, int D, int GT, bool LISTED>
 __global__ __launch_bounds__(kAttendThreads, 3) void paged_attend_kernel(PagedCache c, const T* __restrict__ q, const T* __restrict__ k_new,
                                                                       const T* __restrict__ v_new, int G, PagedStepPlan p, char* ws) {
     using A = WaveAttend<T, D>;
@@ -377,7 +430,7 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_attend_kernel(PagedCa
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, j = lane >> 4;
     constexpr int kStep = A::kBlock * kAttendWaves;
     HeadPart hp;
-    if (!find_head_part(c, p, blockIdx.x, &hp)) return;
+    if (!find_head_part<LISTED>(c, p, ws, blockIdx.x, &hp)) return;
     const int h = hp.h;
     A a;
     a.reset();
@@ -452,12 +505,8 @@ __global__ __launch_bounds__(kAttendThreads, 3) void paged_attend_kernel(PagedCa
 // Joins the parts.  The first n_chunks workgroups of a head take 1024 rows at a time and add their weights to cum; the rest take a share
 // of the outputs, several threads to four features of them; the first also writes the new row.
 template <typename T, int D, int GT, bool POOL>
-__global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache c, const T* __restrict__ k_new, const T* __restrict__ v_new,
-                                                                      const int32_t* __restrict__ pos, int G, int n_chunks, int n_join,
-                                                                      PagedStepPlan p, const char* __restrict__ ws, float* __restrict__ out) {
-    __shared__ float2 norm[16];
-    __shared__ f32x4_t sum_s[kFinishThreads];
-    const int h = blockIdx.x / (n_chunks + n_join), task = blockIdx.x % (n_chunks + n_join);
+__device__ __forceinline__ void finish_task(const PagedCache& c, const T* k_new, const T* v_new, const int32_t* pos, int G, int n_chunks, int n_join,
+                                            const PagedStepPlan& p, const char* ws, float* out, int h, int task, float2* norm, f32x4_t* sum_s) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int4 head = reinterpret_cast<const int4*>(ws + p.head_off)[h];
     const int n = head.x, n1 = head.y, n_parts = head.w;
@@ -530,6 +579,24 @@ __global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache
         float* to = out + (int64_t)h * G * D + quad * 4;
 #pragma unroll
         for (int i = 0; i < 4; ++i) to[i] = o[i] * norm[quad * 4 / D].y;
+    }
+}
+
+template <typename T, int D, int GT, bool POOL, bool LISTED>
+__global__ __launch_bounds__(kFinishThreads) void paged_finish_kernel(PagedCache c, const T* __restrict__ k_new, const T* __restrict__ v_new,
+                                                                      const int32_t* __restrict__ pos, int G, int n_chunks, int n_join,
+                                                                      PagedStepPlan p, const char* __restrict__ ws, float* __restrict__ out) {
+    __shared__ float2 norm[16];
+    __shared__ f32x4_t sum_s[kFinishThreads];
+    const int per = n_chunks + n_join;
+    if constexpr (LISTED) {
+        const int32_t* list = reinterpret_cast<const int32_t*>(reinterpret_cast<const int64_t*>(ws + p.list_off) + 1);
+        for (int task = blockIdx.x, end = list[0] * per; task < end; task += gridDim.x) {
+            finish_task<T, D, GT, POOL>(c, k_new, v_new, pos, G, n_chunks, n_join, p, ws, out, list[1 + task / per], task % per, norm, sum_s);
+            __syncthreads();
+        }
+    } else {
+        finish_task<T, D, GT, POOL>(c, k_new, v_new, pos, G, n_chunks, n_join, p, ws, out, blockIdx.x / per, blockIdx.x % per, norm, sum_s);
     }
 }
 
@@ -950,8 +1017,12 @@ size_t head_step_lds(int G, int D, int rows) {
 PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows, int64_t pool_rows) {
     PagedStepPlan p{};
     p.rows = (rows + 31) / 32 * 32;                                       // whole blocks are written
-    p.one_launch = n_heads >= kHeadLaunchHeads && head_step_lds(G, D, p.rows) <= kHeadLaunchLds;
-    if (p.one_launch) return p;
+    if (n_heads >= kHeadLaunchHeads) {
+        p.split = head_step_lds(G, D, p.rows) > kHeadLaunchLds;
+        p.head_rows = p.split ? (int)(kShortHeadLds / (heads_bound(G) * sizeof(float))) / 32 * 32 : p.rows;
+        if (!p.split) return p;
+    }
+    p.split = true;
     const int64_t units = (int64_t)n_heads * ((rows + kLeastShare - 1) / kLeastShare);
     // broken parts count half: together about as many as run at a time; of more heads than that, several rounds
     const int aim = n_heads < kHeadLaunchHeads ? kSplitAim - n_heads / 2 : 4 * kSplitAim;
@@ -964,6 +1035,7 @@ PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows, int64_t pool_
         return at;
     };
     p.by_pool = 2 * pool_rows < (int64_t)n_heads * p.rows;
+    p.list_off = take(sizeof(int64_t) + ((size_t)n_heads + 1) * sizeof(int32_t));
     p.head_off = take((size_t)n_heads * sizeof(int4));
     p.ml_off = take(parts * G * sizeof(float2));
     p.acc_off = take(parts * G * D * sizeof(float));
@@ -1013,26 +1085,35 @@ hipError_t step_of(const PagedCache& c, const void* q, const void* k_new, const 
                    char* ws, float* out, const Env& env) {
     const T* kn = static_cast<const T*>(k_new);
     const T* vn = static_cast<const T*>(v_new);
-    if (p.one_launch) {
-        env.begin("paged_head");
-        paged_head_kernel<T, D, GT><<<c.n_heads, kAttendThreads, head_step_lds(G, D, p.rows), env.s>>>(c, static_cast<const T*>(q), kn, vn, pos, G,
-                                                                                                       p.rows, out);
+    if (p.split && p.head_rows > 0) {
+        env.begin("paged_list");
+        paged_list_kernel<<<1, 1024, 0, env.s>>>(c, p.head_rows, p, ws);
         env.end();
-        return hipGetLastError();
     }
+    if (p.head_rows > 0) {
+        env.begin("paged_head");
+        paged_head_kernel<T, D, GT><<<c.n_heads, kAttendThreads, head_step_lds(G, D, p.head_rows), env.s>>>(c, static_cast<const T*>(q), kn, vn, pos,
+                                                                                                            G, p.head_rows, p.split, out);
+        env.end();
+    }
+    if (!p.split) return hipGetLastError();
+    const bool listed = p.head_rows > 0;
     env.begin("paged_attend");
-    paged_attend_kernel<T, D, GT><<<p.n_split + c.n_heads, kAttendThreads, (size_t)kAttendWaves * G * D * sizeof(float), env.s>>>(
-        c, static_cast<const T*>(q), kn, vn, G, p, ws);
+    const auto attend = listed ? paged_attend_kernel<T, D, GT, true> : paged_attend_kernel<T, D, GT, false>;
+    attend<<<p.n_split + c.n_heads, kAttendThreads, (size_t)kAttendWaves * G * D * sizeof(float), env.s>>>(c, static_cast<const T*>(q), kn, vn, G, p, ws);
     env.end();
-    // a workgroup joins up to 64 KiB of partial outputs, of at most as many quads as it has threads
-    const int n_chunks = min((p.rows + kFinishRows - 1) / kFinishRows, kFinishWgs / c.n_heads + 1);
-    const int n_parts = (p.n_split + c.n_heads - 1) / c.n_heads;
-    int n_join = (int)(((int64_t)n_parts * G * D * 4 + 65535) / 65536);
-    const int least = (G * D / 4 + kFinishThreads - 1) / kFinishThreads;
-    n_join = out == nullptr ? 0 : n_join < least ? least : n_join;
+    // a workgroup joins up to 64 KiB of partial outputs, of at most as many quads as it has threads; 16 quads, if heads are listed: one may have all
+    // parts
+    const int n_chunks = (p.rows + kFinishRows - 1) / kFinishRows, most_chunks = listed ? 128 : kFinishWgs / c.n_heads + 1;
+    const int chunks = min(n_chunks, most_chunks), n_parts = (p.n_split + c.n_heads - 1) / c.n_heads;
+    int n_join = listed ? G * D / 64 : (int)(((int64_t)n_parts * G * D * 4 + 65535) / 65536);
+    n_join = max(n_join, (G * D / 4 + kFinishThreads - 1) / kFinishThreads);
+    if (out == nullptr) n_join = 0;
+    const int64_t tasks = (int64_t)c.n_heads * (chunks + n_join);
     env.begin("paged_finish");
-    const auto finish = p.by_pool ? paged_finish_kernel<T, D, GT, true> : paged_finish_kernel<T, D, GT, false>;
-    finish<<<c.n_heads * (n_chunks + n_join), kFinishThreads, 0, env.s>>>(c, kn, vn, pos, G, n_chunks, n_join, p, ws, out);
+    const auto finish = p.by_pool ? listed ? paged_finish_kernel<T, D, GT, true, true> : paged_finish_kernel<T, D, GT, true, false>
+                                  : listed ? paged_finish_kernel<T, D, GT, false, true> : paged_finish_kernel<T, D, GT, false, false>;
+    finish<<<(int)(listed ? min(tasks, (int64_t)kFinishWgs) : tasks), kFinishThreads, 0, env.s>>>(c, kn, vn, pos, G, chunks, n_join, p, ws, out);
     env.end();
     return hipGetLastError();
 }

@@ -176,6 +176,37 @@ def test_queries_alone_missing_pages_and_lengths_out_of_range(ctx, dtype):
     assert np.array_equal(state[0][int(c.table[0, 5])], raw_bits(c.K[int(c.table[0, 5])]))
 
 
+@pytest.mark.parametrize("n,G,D,dtype,max_pages", [(520, 4, 128, torch.bfloat16, 80), (600, 16, 64, torch.float32, 40), (700, 8, 128, torch.bfloat16, 200)])
+def test_many_heads_short_and_long(ctx, n, G, D, dtype, max_pages):
+    """Short heads, and among them some too long for one workgroup's LDS, at lengths around that (50 KiB of logits), none of them and all of them."""
+    page = 64
+    short = 50 * 1024 // (G * 4) // 32 * 32
+    lens = [(37 * h) % 90 for h in range(n)]
+    long = {0: short - 2, 1: short - 1, 2: short, 3: short + 1, 70: min(2 * short, max_pages * page - 3), n // 2: short + 40, n - 1: short + 130}
+    for h, m in long.items():
+        lens[h] = m
+    c, _ = _cache(ctx, lens, page, max_pages, D, dtype, 42, room=3)
+    pick = sorted(long) + [4, 5, 69, 71, n - 2]
+    for t in range(3):                                                   # (the third without the new token)
+        q, kn, vn = _token(n, G, D, dtype, 60 + t)
+        before = {h: _rows(c, h) for h in pick}
+        pos = torch.full((n,), 10 ** 6 + t, dtype=torch.int32, device=DEV)
+        out = ctx.paged_step(c, q.to(DEV), kn.to(DEV), vn.to(DEV), pos) if t < 2 else ctx.paged_step(c, q.to(DEV))
+        torch.cuda.synchronize()
+        assert c.length.cpu().tolist() == [m + min(t + 1, 2) for m in lens]
+        for h in pick:
+            _check_step(before[h], _rows(c, h), q[h], kn[h] if t < 2 else None, vn[h], 10 ** 6 + t, out[h].cpu(), dtype, f"token {t}, head {h}")
+    c.length.zero_()
+    assert (ctx.paged_step(c, q.to(DEV)) == 0).all() and (c.length == 0).all()
+    if G == 16:
+        c, _ = _cache(ctx, [short + h % 3 for h in range(n)], page, max_pages, D, dtype, 43)
+        before = {h: _rows(c, h) for h in pick}
+        out = ctx.paged_step(c, q.to(DEV))
+        torch.cuda.synchronize()
+        for h in pick:
+            _check_step(before[h], _rows(c, h), q[h], None, None, 0, out[h].cpu(), dtype, f"all long, head {h}")
+
+
 @pytest.mark.parametrize("n,G,max_pages,mib", [(6, 4, 2500, 3), (100, 16, 600, 8), (700, 8, 2500, 24)])
 def test_tables_with_more_room_than_the_pool_has_rows(ctx, n, G, max_pages, mib):
     """Tables for thousands of rows a head over a pool of a few pages each: the workspace goes by the pool.  Steps and evictions; a head that counts
