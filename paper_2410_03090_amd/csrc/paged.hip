@@ -763,10 +763,11 @@ __device__ Cut last_of_smallest(F&& each, int want, int* hist, int* buf, uint32_
 }
 }  // namespace
 
-// Short tables (at most 64 R rows): a wave per head with every row's key in a register; nobody waits for anybody.  Whole evictions, us: 5120 heads
+// Short heads (at most 64 R rows): a wave per head with every row's key in a register; nobody waits for anybody.  Whole evictions, us: 5120 heads
 // of 720 rows, an eighth of them without weight, 150 (274 with the cut found bit by bit, by counts of the keys below it).  By a wave and by
 // a workgroup per head: 8 heads of 1900 rows 46 / 29, 256 heads 62 / 48, 2000 heads 116 / 202.
-template <int R>
+// Where tables of many heads have room for more, the short heads are seen to first (5120 heads of 700 rows, room for 8192, 150; all by workgroups 259).
+template <int R, bool POOL>
 __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos,
                                                                 int w, PagedEvictPlan p, char* ws, int32_t* __restrict__ evicted) {
     __shared__ __align__(16) int hist_s[4][256];
@@ -774,7 +775,8 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
     if (wg >= c.n_heads) return;
     const int h = spread_head(wg, c.n_heads), n = head_rows(c, h), over = rows_over(n, budget[h], w);
     const int64_t newest = (int64_t)pos[h] - w;
-    int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off) + (int64_t)h * p.rows;          // (never by the pool)
+    if (n > 64 * R) return;                                               // a workgroup's
+    int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off);
     const int32_t* table = c.table + (int64_t)h * c.max_pages;
     const int in_page = (1 << c.shift) - 1;
     int drop = 0, gaps = 0;
@@ -836,8 +838,8 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
             const int r = 64 * i + lane;
             const bool out = leaves >> i & 1, gap = out && r < stay, mover = !out && r >= stay && r < n;
             const unsigned long long g = __ballot(gap), m = __ballot(mover), lower = (1ull << lane) - 1;
-            if (gap) pairs[gaps + __builtin_popcountll(g & lower)].x = at[i];
-            if (mover) pairs[movers + __builtin_popcountll(m & lower)].y = at[i];
+            if (gap) pairs[row_entry<POOL>(c, h, gaps + __builtin_popcountll(g & lower))].x = at[i];
+            if (mover) pairs[row_entry<POOL>(c, h, movers + __builtin_popcountll(m & lower))].y = at[i];
             gaps += __builtin_popcountll(g);
             movers += __builtin_popcountll(m);
         }
@@ -866,10 +868,10 @@ __global__ __launch_bounds__(256) void paged_key_kernel(PagedCache c, const int3
         }
 }
 
-// Longer tables: a workgroup per head, keys in LDS where they fit and from the workspace otherwise, four at a time.
+// Longer heads: a workgroup per head, keys in LDS where they fit and from the workspace otherwise, four at a time.
 template <bool POOL>
 __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos,
-                                                                      int w, PagedEvictPlan p, char* ws, int32_t* __restrict__ evicted) {
+                                                                      int w, PagedEvictPlan p, int least, char* ws, int32_t* __restrict__ evicted) {
     extern __shared__ __align__(16) uint32_t key_s[];
     __shared__ int hist[kSelectThreads];
     __shared__ int buf[kSelectThreads / 64];
@@ -877,6 +879,7 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache
     __shared__ int pick[3];
     const int h = spread_head(blockIdx.x, gridDim.x), tid = threadIdx.x;
     const int n = head_rows(c, h), over = rows_over(n, budget[h], w);
+    if (n < least) return;                                                // a wave has seen to it
     const int64_t newest = (int64_t)pos[h] - w;
     int2* pairs = reinterpret_cast<int2*>(ws + p.pair_off);
     const bool in_lds = p.keys_in_lds;
@@ -1157,21 +1160,26 @@ hipError_t launch_paged_evict(const PagedCache& c, const int32_t* budget, const 
     env.begin("paged_select");
     const int rows = c.max_pages << c.shift;
     const unsigned by_wave = (unsigned)(c.n_heads + 3) / 4;
-    const auto wave_form = [&](auto r) {
-        paged_select_wave_kernel<decltype(r)::value><<<by_wave, 256, 0, env.s>>>(c, budget, pos, w, p, ws, evicted);
+    const auto wave_form = [&](auto r, auto pool) {
+        paged_select_wave_kernel<decltype(r)::value, decltype(pool)::value><<<by_wave, 256, 0, env.s>>>(c, budget, pos, w, p, ws, evicted);
     };
-    const int least = c.n_heads > kWaveSelectHeads ? 64 * 32 : 64 * 16;   // rows up to which a wave per head is the faster form
-    if (rows <= 64 * 8) wave_form(std::integral_constant<int, 8>{});
-    else if (rows <= 64 * 16) wave_form(std::integral_constant<int, 16>{});
-    else if (rows <= 64 * 24 && rows <= least) wave_form(std::integral_constant<int, 24>{});
-    else if (rows <= 64 * kWaveSelectRows && rows <= least) wave_form(std::integral_constant<int, kWaveSelectRows>{});
+    constexpr std::false_type kTable{};
+    constexpr std::true_type kPool{};
+    constexpr std::integral_constant<int, kWaveSelectRows> kMost{};
+    const bool many = c.n_heads > kWaveSelectHeads;
+    const int least = many ? 64 * kWaveSelectRows : 64 * 16;              // rows up to which a wave per head is the faster form
+    if (rows <= 64 * 8) wave_form(std::integral_constant<int, 8>{}, kTable);
+    else if (rows <= 64 * 16) wave_form(std::integral_constant<int, 16>{}, kTable);
+    else if (rows <= 64 * 24 && rows <= least) wave_form(std::integral_constant<int, 24>{}, kTable);
+    else if (rows <= least) wave_form(kMost, kTable);
     else {
+        if (many) p.by_pool ? wave_form(kMost, kPool) : wave_form(kMost, kTable);
         if (!p.keys_in_lds) {
             const int most = (rows + 1023) / 1024, n_chunks = min(most, (4096 + c.n_heads - 1) / c.n_heads);
             paged_key_kernel<<<c.n_heads * n_chunks, 256, 0, env.s>>>(c, budget, pos, w, p, n_chunks, ws);
         }
         const auto select = p.by_pool ? paged_select_kernel<true> : paged_select_kernel<false>;
-        select<<<c.n_heads, kSelectThreads, p.keys_in_lds ? (size_t)(rows + 3) / 4 * 16 : 0, env.s>>>(c, budget, pos, w, p, ws, evicted);
+        select<<<c.n_heads, kSelectThreads, p.keys_in_lds ? (size_t)(rows + 3) / 4 * 16 : 0, env.s>>>(c, budget, pos, w, p, many ? least + 1 : 0, ws, evicted);
     }
     env.end();
     int n_chunks = 2048 / c.n_heads;

@@ -336,6 +336,20 @@ def _check_evict(ctx, c, budget, pos, w):
             assert np.array_equal(raw_bits(a), raw_bits(b[order])), h
 
 
+@pytest.mark.parametrize("max_pages", [64, 1100])
+def test_evict_short_and_long_heads_together(ctx, max_pages):
+    """More heads than get a workgroup each, lengths around what a wave keeps in its registers; tables with room for 4096 rows and for 70400."""
+    n, page = 520, 64
+    lens = [(53 * h) % 120 for h in range(n)]
+    for i, m in enumerate((2046, 2047, 2048, 2049, 2050, 3000, 4000)):
+        lens[71 * i] = m
+    c, _ = _cache(ctx, lens, page, max_pages, 64, torch.bfloat16, 44)
+    budget = [m // 2 + h % 3 for h, m in enumerate(lens)]
+    pos = [4 * max(lens) if h % 5 else 200 for h in range(n)]            # (few rows old enough in some)
+    _check_evict(ctx, c, budget, pos, 4)
+    _check_evict(ctx, c, [b // 2 for b in budget], pos, 2)
+
+
 @pytest.mark.parametrize("lens", [[1016, 200, 65, 700], [1016, 200, 1400, 1500], [2600, 700, 129, 2000]])
 def test_evict_of_rows_that_are_all_alike(ctx, lens):
     """One score and one position for hundreds of rows, more than a lane's or a thread's: the first rows leave, down to the budget exactly."""
