@@ -418,7 +418,12 @@ uncomp_status uncomp_budgets_from_labels(uncomp_ctx* ctx, const int32_t* labels,
  * and lengths are cut to them.  Rows of out / lse_out that belong to no sequence are left alone; key
  * rows may be shared by sequences, query rows may not.
  * Strides are multiples of 8 elements, none negative, row strides >= D; Q, K, V and out 16-byte aligned;
- * D 64 or 128; q_rows*G <= 2^30.  Workspace: uncomp_prefill_attention_workspace_bytes.
+ * row strides of K and V below 2^24 elements; D 64 or 128; q_rows*G and k_rows <= 2^30; n_seq <= 65536.
+ * Up to 64 sequences share the longest tiles out first; more are taken in their order.
+ * Workspace: uncomp_prefill_attention_workspace_bytes for the best speed.  Long tiles are cut into
+ * parts where the context's workspace holds those (results then differ in their last bits); only more
+ * than 64 sequences need workspace, 8 bytes each.  uncomp_set_kernel_path does not concern this call
+ * and the paged ones, which have no plain-ALU form.
  */
 size_t uncomp_prefill_attention_workspace_bytes(int n_seq, int H, int G, int D, int q_rows, int k_rows);
 uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const void* K, const void* V,

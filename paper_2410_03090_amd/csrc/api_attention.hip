@@ -121,8 +121,10 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
         a.lse_sh = lse_strides[1];
     }
     if (!prefill_attention_fits(a, dtype, D)) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
-    // what the call leaves in the workspace is as much as fits there
-    uncomp_status st = take_workspace(ctx, who, ctx->ws_bytes, stream);
+    // (beyond that, what the call leaves in the workspace is as much as fits there)
+    uncomp_status st = take_workspace(ctx, who, prefill_attention_least_bytes(n_seq), stream);
+    if (st != UNCOMP_OK) return st;
+    st = take_workspace(ctx, who, ctx->ws_bytes, stream);
     if (st != UNCOMP_OK) return st;
     OnDevice on(ctx->device);
     if (on.err != hipSuccess) return hip_fail(ctx, on.err, who);

@@ -326,8 +326,10 @@ struct PrefillArgs {
     unsigned items;      // tiles of all KV heads, at most
     float2* part_ml;     // where parts leave (maximum, sum) and outputs
     float* part_acc;
+    int64_t* sums;       // tiles of the sequences up to each, where there are many
 };
 bool prefill_attention_fits(const PrefillArgs& a, uncomp_dtype dt, int D);       // the launch's grid
+size_t prefill_attention_least_bytes(int n_seq);                                 // without which it does not run
 size_t prefill_attention_bytes(int n_seq, int H, int G, int D, int q_rows, int k_rows);
 hipError_t launch_prefill_attention(const PrefillArgs& a, uncomp_dtype dt, int D, char* ws, size_t ws_bytes, const Env& env);
 

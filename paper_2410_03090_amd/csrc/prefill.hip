@@ -25,6 +25,7 @@ __device__ __forceinline__ void rows_of(const AttnRows& r, int s, int* first, in
 // sequence see ever more keys, so how many see at least x blocks is a subtraction, and x is found by bisection, 64 sequences at a time.
 // Returns whether there is such a tile; called by whole waves, the same for all lanes.  blocks: those of all tiles (a tile sees
 // about the mean of its sequence's first and last), 0 with more than 64 sequences, which are taken in their order.
+constexpr int kRanked = 64;
 struct Tile {
     int seq, tile, q_first, nq, k_first, nk;
     int64_t blocks;
@@ -62,7 +63,7 @@ __device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile, int64_
         *out = Tile{0, n - 1 - (int)rank, qf, nq, kf, nk, (int64_t)n * (first + nk) / 128};
         return rank < n;
     }
-    if (a.n_seq <= 64) {
+    if (a.n_seq <= kRanked) {
         seq_of(lane, &qf, &nq, &kf, &nk);
         const int n = tiles_of(nq);
         if (rank >= wave_total(n)) return false;
@@ -96,30 +97,20 @@ __device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile, int64_
         out->nk = __shfl(nk, x, 64);
         return true;
     }
-    // many sequences: in their order
-    for (int s0 = 0; s0 < a.n_seq; s0 += 64) {
-        seq_of(s0 + lane, &qf, &nq, &kf, &nk);
-        const int n = tiles_of(nq);
-        int sum = n;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int u = __shfl_up(sum, o, 64);
-            if (lane >= o) sum += u;
-        }
-        const unsigned long long has = __ballot(sum > rank);
-        if (has != 0) {
-            const int x = __ffsll(has) - 1;
-            out->tile = __shfl(n - sum + (int)rank, x, 64);
-            out->seq = s0 + x;
-            out->q_first = __shfl(qf, x, 64);
-            out->nq = __shfl(nq, x, 64);
-            out->k_first = __shfl(kf, x, 64);
-            out->nk = __shfl(nk, x, 64);
-            return true;
-        }
-        rank -= __shfl(sum, 63, 64);
+    // many sequences: in their order, found among the sums of their tiles, 64 places of a range at a time
+    int begin = 0, n = a.n_seq;                                           // the sequence is one of these
+    if (rank >= a.sums[n - 1]) return false;
+    while (n > 1) {
+        const int step = (n + 63) / 64, end = min((lane + 1) * step, n);
+        const int x = __ffsll(__ballot(a.sums[begin + end - 1] > rank)) - 1;
+        begin += x * step;
+        n = min(step, n - x * step);
     }
-    return false;
+    rows_of(a.q, begin, &qf, &nq);
+    rows_of(a.k, begin, &kf, &nk);
+    const int64_t sum = a.sums[begin];
+    *out = Tile{begin, tiles_of(nq) - (int)(sum - rank), qf, nq, kf, nk, 0};
+    return true;
 }
 
 constexpr int kWaveCols = 64;      // columns of a workgroup of the fp32 kernel: sixteen a wave
@@ -177,6 +168,33 @@ __device__ __forceinline__ int64_t part_row(const PrefillArgs& a, int tile, int 
 }
 
 }  // namespace
+
+// Sums of the sequences' tiles, for many of them.  One workgroup, a run of sequences a thread.
+__global__ __launch_bounds__(1024) void prefill_sums_kernel(AttnRows q, int n_seq, int G, int tile, int64_t* __restrict__ sums) {
+    __shared__ int64_t wave_s[16];
+    const int tid = threadIdx.x, lane = tid & 63, run = (n_seq + 1023) / 1024, begin = min(n_seq, tid * run), end = min(n_seq, begin + run);
+    const auto tiles = [&](int s) {
+        int first, n;
+        rows_of(q, s, &first, &n);
+        return (n * G + tile - 1) / tile;
+    };
+    int64_t mine = 0;
+    for (int s = begin; s < end; ++s) mine += tiles(s);
+    int64_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t u = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += u;
+    }
+    if (lane == 63) wave_s[tid >> 6] = sum;
+    __syncthreads();
+    sum -= mine;
+    for (int x = 0; x < tid >> 6; ++x) sum += wave_s[x];
+    for (int s = begin; s < end; ++s) {
+        sum += tiles(s);
+        sums[s] = sum;
+    }
+}
 
 // ---- fp32 ------------------------------------------------------------------------------------------------------------
 // Sixteen columns per wave, rows straight from memory into the operands: the fp32 matrix cores take 2048 cycles for sixteen rows of
@@ -558,8 +576,8 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(
     }
     const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     l = __uint_as_float(other[0]) + __uint_as_float(other[1]);
-    if (col > w.last_col) return;
     if (w.n_parts > 1) {
+        if (col > w.last_col) return;
         const int64_t row = part_row(a, kCols, col - w.c0);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
@@ -570,8 +588,13 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(
         return;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    bf16_bits* O = static_cast<bf16_bits*>(a.out) + w.s * a.o.ss + head * a.o.sh + (int64_t)(w.q_first + qi) * a.o.sr;
+    if (a.lse != nullptr && half == 0 && col <= w.last_col)
+        a.lse[w.s * a.lse_ss + head * a.lse_sh + w.q_first + qi] = l == 0.f ? -INFINITY : (m * scale2 + log2f(l)) * kLn2A;
+    // a lane's four features are eight bytes: whole rows are put together in the buffers, a wave's 32 in a part of its own
+    arrived();
     typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+    constexpr int kFit = kTileBytes / (32 * kRowBytes);
+    unsigned char* mine = (wave / kFit == 0 ? keys0 : wave / kFit == 1 ? keys1 : wave / kFit == 2 ? values0 : values1) + wave % kFit * 32 * kRowBytes;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -579,10 +602,20 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(
             bf16x4_t v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = (__bf16)(o[b][r + e] * inv);
-            *reinterpret_cast<bf16x4_t*>(O + 32 * b + 2 * r + 4 * half) = v;
+            *reinterpret_cast<bf16x4_t*>(mine + c * kRowBytes + ((4 * b + r / 4) ^ (c & (kPieces - 1))) * 16 + 8 * half) = v;
         }
-    if (a.lse != nullptr && half == 0)
-        a.lse[w.s * a.lse_ss + head * a.lse_sh + w.q_first + qi] = l == 0.f ? -INFINITY : (m * scale2 + log2f(l)) * kLn2A;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    bf16_bits* O = static_cast<bf16_bits*>(a.out) + w.s * a.o.ss + (int64_t)w.q_first * a.o.sr;
+    const int64_t to = head * a.o.sh + qi * a.o.sr;
+#pragma unroll
+    for (int i = 0; i < kPieces / 2; ++i) {
+        const int row = i * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
+        const int64_t at = __shfl(to, row);
+        if (c_wave + row <= w.last_col)
+            *reinterpret_cast<u32x4_t*>(O + at + 8 * piece) = *reinterpret_cast<const u32x4_t*>(mine + row * kRowBytes + (piece ^ (row & (kPieces - 1))) * 16);
+    }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -595,41 +628,63 @@ struct Plan {
 };
 // 64-wide heads take tiles of 128 columns, two workgroups a CU: as much work for the vector unit comes with half the products, and
 // two that do not wait for each other fill it better (8 KV heads of 1024 rows 28.5 -> 22.3 us, 8192 rows 357 -> 347).
-Plan plan(bool f32, bool packed, int n_seq, int H, int G, int D, int q_rows, int k_rows) {
+// 128-wide ones take tiles of 256, which read keys and values half as often, unless a sequence has not as many columns, or its keys are soon
+// through (what comes before and after them then counts, and another workgroup fills it), or they would not fill the chip.  256 / 128, us, 8
+// KV heads of 4 query heads: 16 sequences of 1 query on 20000 keys 341 / 199, 256 prompts of 128 rows 280 / 248, 32 of 1024 455 / 444, 1 of 1024
+// 35.6 / 29.0, 1 of 2048 66.5 / 67.6, 32 of 2048 1354 / 1408, 4 times 512 on 16000 484 / 519; of 1 query head, 1 of 4096 98 / 70, 4 of 4096 152 / 166.
+constexpr int kShortKeys = 1536;
+int tile_of(bool f32, bool q_packed, bool k_packed, int n_seq, int H, int G, int D, int q_rows, int k_rows) {
+    if (f32) return kWaveCols;
+    const int64_t cols = (int64_t)q_rows * G / (q_packed ? n_seq : 1), keys = k_rows / (k_packed ? n_seq : 1);      // of a sequence, on the average
+    const int64_t tiles = (cols + 255) / 256 * n_seq * H;
+    return D == 64 || cols <= 128 || keys <= kShortKeys || (tiles < 256 && keys < 2 * cols / G) ? 128 : 256;
+}
+Plan plan(int tile, bool packed, int n_seq, int H, int G, int D, int q_rows, int k_rows) {
     const int64_t cols = (int64_t)q_rows * G;
     Plan p;
-    p.tile = f32 ? kWaveCols : D == 64 ? 128 : 256;
-    p.target = p.tile == 256 ? 256 : f32 ? 512 : 768;                                 // workgroups that run at a time
+    p.tile = tile;
+    const bool f32 = tile == kWaveCols;
+    p.target = tile == 256 ? 256 : f32 || D == 128 ? 512 : 768;                       // workgroups that run at a time
     p.least = f32 ? kLeastBlocksF32 : kLeastBlocks;
     // most tiles that the sequences can have: whole ones, and one broken one each
     p.items = (packed ? cols / p.tile + n_seq : (cols + p.tile - 1) / p.tile * n_seq) * H;
     // as if the rows were one sequence's; how they are divided only the device knows
     const int64_t most = ((int64_t)k_rows + 63) / 64, first = (k_rows > q_rows ? (int64_t)k_rows - q_rows : 0) / 64;
-    p.n_split = n_seq > 64 ? 1 : parts_of(most, p.items * (first + most + 1) / 2, p.target, p.least, 64);
+    p.n_split = n_seq > kRanked ? 1 : parts_of(most, p.items * (first + most + 1) / 2, p.target, p.least, 64);
     p.acc_off = align_up((size_t)p.items * p.n_split * p.tile * sizeof(float2), 256);
-    p.bytes = p.n_split == 1 ? 0 : p.acc_off + (size_t)p.items * p.n_split * p.tile * D * sizeof(float);
+    p.bytes = n_seq > kRanked ? (size_t)n_seq * sizeof(int64_t) : p.n_split == 1 ? 0 : p.acc_off + (size_t)p.items * p.n_split * p.tile * D * sizeof(float);
     return p;
+}
+Plan plan(const PrefillArgs& a, bool f32, int D) {
+    const bool packed = a.q.first != nullptr;
+    return plan(tile_of(f32, packed, a.k.first != nullptr, a.n_seq, a.H, a.G, D, a.q.rows, a.k.rows), packed, a.n_seq, a.H, a.G, D, a.q.rows, a.k.rows);
 }
 }  // namespace
 
 size_t prefill_attention_bytes(int n_seq, int H, int G, int D, int q_rows, int k_rows) {
     size_t most = 0;
-    for (int i = 0; i < 4; ++i) {
-        const size_t b = plan(i & 1, i & 2, n_seq, H, G, D, q_rows, k_rows).bytes;
-        most = b > most ? b : most;
-    }
+    for (int tile : {kWaveCols, 128, 256})
+        for (bool packed : {false, true}) {
+            const size_t b = plan(tile, packed, n_seq, H, G, D, q_rows, k_rows).bytes;
+            most = b > most ? b : most;
+        }
     return most;
 }
 
-bool prefill_attention_fits(const PrefillArgs& a, uncomp_dtype dt, int D) {
-    return plan(dt == UNCOMP_F32, a.q.first != nullptr, a.n_seq, a.H, a.G, D, a.q.rows, a.k.rows).items <= (1 << 30) / 16;
-}
+bool prefill_attention_fits(const PrefillArgs& a, uncomp_dtype dt, int D) { return plan(a, dt == UNCOMP_F32, D).items <= (1 << 30) / 16; }
+size_t prefill_attention_least_bytes(int n_seq) { return n_seq > kRanked ? (size_t)n_seq * sizeof(int64_t) : 0; }
 
 namespace {
 template <int D>
 hipError_t prefill_of(PrefillArgs a, bool f32, char* ws, size_t ws_bytes, const Env& env) {
-    Plan p = plan(f32, a.q.first != nullptr, a.n_seq, a.H, a.G, D, a.q.rows, a.k.rows);
+    Plan p = plan(a, f32, D);
     if (p.bytes > ws_bytes) p.n_split = 1;                               // no room for parts: whole tiles
+    if (a.n_seq > kRanked) {
+        a.sums = reinterpret_cast<int64_t*>(ws);
+        env.begin("prefill_sums");
+        prefill_sums_kernel<<<1, 1024, 0, env.s>>>(a.q, a.n_seq, a.G, p.tile, a.sums);
+        env.end();
+    }
     a.n_split = p.n_split;
     a.target = p.target;
     a.least = p.least;
@@ -643,8 +698,8 @@ hipError_t prefill_of(PrefillArgs a, bool f32, char* ws, size_t ws_bytes, const 
         env.end();
     } else {
         env.begin("prefill_tile");
-        constexpr int kWaves = D == 64 ? 4 : 8;
-        prefill_tile_kernel<D, kWaves><<<grid, 64 * kWaves, 0, env.s>>>(a);
+        if (p.tile == 128) prefill_tile_kernel<D, 4><<<grid, 256, 0, env.s>>>(a);
+        else if constexpr (D == 128) prefill_tile_kernel<D, 8><<<grid, 512, 0, env.s>>>(a);
         env.end();
     }
     hipError_t e = hipGetLastError();

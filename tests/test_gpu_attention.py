@@ -176,6 +176,75 @@ def test_shared_keys_starts_out_of_range_and_many_sequences(ctx):
     _check_packed(Q, K, V, G, qs, ks, out, lse, torch.bfloat16)
 
 
+@pytest.mark.parametrize("n,most,D,dtype", [(65, 40, 128, torch.bfloat16), (200, 90, 64, torch.bfloat16), (1500, 12, 128, torch.bfloat16),
+                                            (4200, 5, 64, torch.float32), (4097, 3, 128, torch.bfloat16)])
+def test_many_short_sequences(ctx, n, most, D, dtype):
+    """More sequences than lanes, and than lanes squared, some without queries or keys, a few longer than a tile."""
+    H, G = 1, 4
+    g = torch.Generator().manual_seed(n)
+    q = torch.randint(0, most, (n,), generator=g).tolist()
+    k = [max(0, m + d) for m, d in zip(q, torch.randint(-2, 4, (n,), generator=g).tolist())]
+    for s, m in ((0, 0), (1, 70), (63, 33), (64, 200), (n - 1, 64)):
+        q[s], k[s] = m, m + s % 3
+    Q, K, V, qs, ks = _packed(list(zip(q, k)), H, G, D, dtype, 14)
+    out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
+    _check_packed(Q, K, V, G, qs, ks, out, lse, dtype, heads=[n % G])
+
+
+@pytest.mark.parametrize("H,G,q_rows,k_rows,ws", [(2, 4, 300, 2100, 64 << 20), (2, 4, 300, 2100, 256), (1, 1, 500, 1700, 64 << 20), (3, 7, 40, 4000, 256)])
+def test_wide_tiles_of_columns(ctx, H, G, q_rows, k_rows, ws):
+    """Prompts with room for many more keys than queries, in a padded batch: whole, short, with one row, without, with values that are not finite
+    behind what rows see; with and without room for parts of a tile."""
+    from paper_2410_03090_amd import binding
+    D, dtype = 128, torch.bfloat16
+    q_len = [q_rows, 1, 130, 0, q_rows - 3, 33]
+    k_len = [k_rows, k_rows - 1, 64, 10, q_rows - 3, 31]
+    n = len(q_len)
+    g = torch.Generator().manual_seed(q_rows)
+    q_len = [min(m, q_rows) for m in q_len]
+    Q = (1.3 * torch.randn(n, q_rows, H * G, D, generator=g)).to(dtype).transpose(1, 2)
+    K, V = (torch.randn(n, k_rows, H, D, generator=g).to(dtype).transpose(1, 2) for _ in range(2))
+    for s, m in enumerate(k_len):
+        K[s, :, m:], V[s, :, m:] = float("nan"), float("inf")
+        V[s, :, max(m - 5, 0):m, 3] = float("inf")
+    small = binding.Context(0, ws)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    out = torch.full((n, H * G, q_rows, D), 7.0, dtype=dtype, device=DEV)
+    lse = torch.full((n, H * G, q_rows), 7.0, device=DEV)
+    small.prefill_attention(Q.to(DEV), K.to(DEV), V.to(DEV), G, q_len=i32(q_len), k_len=i32(k_len), out=out, lse=lse)
+    torch.cuda.synchronize()
+    out, lse = out.cpu(), lse.cpu()
+    for s in range(n):
+        assert (out[s, :, q_len[s]:] == 7.0).all() and (lse[s, :, q_len[s]:] == 7.0).all()
+        for h in range(H * G):
+            _check(Q[s, h, :q_len[s]], K[s, h // G, :k_len[s]], V[s, h // G, :k_len[s]], out[s, h, :q_len[s]], lse[s, h, :q_len[s]], dtype,
+                   f"sequence {s}, head {h}")
+    small.close()
+
+
+def test_wide_tiles_of_long_prompts(ctx):
+    """More heads than fill the chip with tiles of 256 columns."""
+    H, G, D, dtype = 40, 1, 128, torch.bfloat16
+    Q, K, V, qs, ks = _packed([(1700, 1700), (900, 3000)], H, G, D, dtype, 15)
+    out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
+    _check_packed(Q, K, V, G, qs, ks, out, lse, dtype, heads=[0, 17, 39])
+
+
+def test_many_sequences_need_workspace(ctx):
+    from paper_2410_03090_amd import binding
+    small = binding.Context(0, 256)
+    for n in (64, 65, 40000):                                             # (a context has some tens of KiB at least)
+        Q, K, V, qs, ks = _packed([(1, 2)] * n, 1, 2, 64, torch.bfloat16, 16)
+        if n <= 65:
+            out, lse = _run_packed(small, Q, K, V, 2, qs, ks)
+            _check_packed(Q, K, V, 2, qs, ks, out, lse, torch.bfloat16, heads=[1])
+        else:
+            with pytest.raises(binding.UncompError, match="workspace"):
+                _run_packed(small, Q, K, V, 2, qs, ks)
+    assert binding.Context.prefill_attention_workspace_bytes(65, 1, 2, 64, 65, 130) == 65 * 8
+    small.close()
+
+
 def test_graph_replays_on_new_contents_and_a_stream_of_its_own(ctx):
     G, D, dtype = 4, 128, torch.bfloat16
     Q, K, V, qs, ks = _packed([(100, 100), (9, 700)], 2, G, D, dtype, 13)
