@@ -418,7 +418,8 @@ uncomp_status uncomp_budgets_from_labels(uncomp_ctx* ctx, const int32_t* labels,
  * and lengths are cut to them.  Rows of out / lse_out that belong to no sequence are left alone; key
  * rows may be shared by sequences, query rows may not.
  * Strides are multiples of 8 elements, none negative, row strides >= D; Q, K, V and out 16-byte aligned;
- * row strides of K and V below 2^24 elements; D 64 or 128; q_rows*G and k_rows <= 2^30; n_seq <= 65536.
+ * row strides of K and V below 2^24 elements; D 64 or 128; q_rows*G and k_rows <= 2^30; n_seq <= 65536;
+ * up to 2^29 query rows times query heads in all.
  * Up to 64 sequences share the longest tiles out first; more are taken in their order.
  * Workspace: uncomp_prefill_attention_workspace_bytes for the best speed.  Long tiles are cut into
  * parts where the context's workspace holds those (results then differ in their last bits); only more
@@ -442,7 +443,7 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
  * what it points to is DEVICE memory owned by the caller.  The caller hands pages out: a page
  * belongs to one head and stands in its table once.  A table entry outside [0, n_pages) is no page;
  * rows there are not attended to and not written.  page is 16, 32, 64, 128 or 256;
- * max_pages*page <= 2^26; n_pages*page < 2^31; D 64 or 128; K_pages and V_pages 16-byte aligned.
+ * max_pages*page <= 2^26; n_pages*page < 2^31; n_heads < 2^22; D 64 or 128; K_pages and V_pages 16-byte aligned.
  * Workspace of the three calls: uncomp_paged_workspace_bytes, rows = max_pages*page; where all tables
  * together have room for more than twice the rows of the pool it goes by the pool, and that much is
  * not needed (the message of UNCOMP_ERR_WORKSPACE says how much is).

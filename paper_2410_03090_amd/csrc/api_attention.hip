@@ -34,6 +34,7 @@ bool strides_ok(const int64_t s[3], int D) {
     return s[0] >= 0 && s[1] >= 0 && s[2] >= D && (s[0] & 7) == 0 && (s[1] & 7) == 0 && (s[2] & 7) == 0;
 }
 
+constexpr int64_t kMostThreads = 0xffffffffLL;      // of a launch, in all
 constexpr int64_t kMostColumns = 1 << 30, kNoPool = INT64_MAX / 4;
 
 // The workspace starts at offset 0: scores' key ranges are overwritten, side-stream work of an earlier call may still use it.
@@ -59,7 +60,7 @@ uncomp_status check_paged(uncomp_ctx* ctx, const char* who, const uncomp_paged_c
     if ((1 << shift) != c->page) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: pages hold 16, 32, 64, 128 or 256 rows", who);
     if ((int64_t)c->max_pages * c->page > 1 << 26) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: more than 2^26 rows per head", who);
     if ((int64_t)c->n_pages * c->page > 0x7fffffffLL) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 rows in the pool", who);
-    if ((int64_t)c->n_heads * 256 > 0x7fffffffLL) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: too many heads", who);
+    if ((int64_t)c->n_heads * 1024 > kMostThreads) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: too many heads", who);
     if (!aligned16(c->K_pages) || !aligned16(c->V_pages)) return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: 16-byte aligned pages required", who);
     if (!aligned4(c->idx_pages) || !aligned4(c->cum_pages) || !aligned4(c->table) || !aligned4(c->len))
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: misaligned pointer in the cache", who);
@@ -154,7 +155,7 @@ uncomp_status uncomp_paged_append(uncomp_ctx* ctx, const uncomp_paged_cache* cac
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: strides must be multiples of 8 elements, none negative, row stride >= D", who);
     if (!aligned16(K) || !aligned16(V) || !aligned4(idx) || !aligned4(cum) || !aligned4(n_rows))
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: 16-byte aligned K and V required", who);
-    if ((int64_t)c.n_heads * (((int64_t)rows + 63) / 64) > 0x7fffffffLL) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
+    if ((int64_t)c.n_heads * (((int64_t)rows + 63) / 64) * 256 > kMostThreads) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
     st = take_workspace(ctx, who, paged_append_bytes(c.n_heads), stream);
     if (st != UNCOMP_OK) return st;
     OnDevice on(ctx->device);

@@ -118,8 +118,8 @@ constexpr int kWaveCols = 64;      // columns of a workgroup of the fp32 kernel:
 // What a tile of columns sees, and the part of it that one workgroup takes.  Where few tiles, or a few long ones, would leave much of
 // the chip idle, tiles are cut into parts of whole blocks of 64 keys, each about the target-th of all blocks but no fewer than
 // kLeastBlocks: a part leaves its outputs in fp32, and joining them takes as long as about that many blocks (fp32: two).  One layer of 8
-// KV heads, 4 query heads each, uncut and cut (us): 1 query on 20000 keys 456 / 45, 64 on 8000 194 / 47, 512 on 16000 386 / 142, a prompt of
-// 3000 142 / 93; a prompt of 1024, in parts of 8 blocks 38 / 41.
+// KV heads, 4 query heads each, uncut and cut (us): 1 query on 20000 keys 387 / 42, 64 on 8000 203 / 49, 512 on 16000 399 / 150, a prompt of
+// 3000 101 / 99.
 // Key numbers below are counted from the part's first.
 constexpr int kLeastBlocks = 12, kLeastBlocksF32 = 2;
 __host__ __device__ inline int parts_of(int64_t blocks, int64_t all_blocks, int target, int least, int most) {
@@ -322,8 +322,8 @@ __global__ __launch_bounds__(256) void prefill_join_kernel(PrefillArgs a, int ti
 }
 
 // ---- bf16 tiles ------------------------------------------------------------------------------------------------------
-// NW waves of 32 columns each over tiles of 64 keys that the workgroup stages through LDS (two buffers, one barrier a tile; the
-// next tile's rows wait in registers, the one after is on its way).
+// NW waves of 32 columns each over tiles of 64 keys that the workgroup stages through LDS (two buffers, one barrier a tile; its keys
+// are on their way two turns ahead, its values one).
 //   S^T = K Q^T  (32 x 32 x 16): keys are rows, so a lane has one column and its softmax stays in the lane but for one exchange;
 //                accumulator register r of half h = lane / 32 is key 8 (r / 4) + 4 h + r % 4 of a block of 32;
 //   O^T = V^T P^T: sixteen keys a product, slots 4 h ... of both halves of eight: the weights are the operand as they lie, and
@@ -671,7 +671,7 @@ size_t prefill_attention_bytes(int n_seq, int H, int G, int D, int q_rows, int k
     return most;
 }
 
-bool prefill_attention_fits(const PrefillArgs& a, uncomp_dtype dt, int D) { return plan(a, dt == UNCOMP_F32, D).items <= (1 << 30) / 16; }
+bool prefill_attention_fits(const PrefillArgs& a, uncomp_dtype dt, int D) { return plan(a, dt == UNCOMP_F32, D).items * 512 <= 0xffffffffLL; }
 size_t prefill_attention_least_bytes(int n_seq) { return n_seq > kRanked ? (size_t)n_seq * sizeof(int64_t) : 0; }
 
 namespace {

@@ -308,7 +308,7 @@ def test_refusals(ctx):
                dict(lse=out.data_ptr(), ls=c2(0, -1)), dict(lse=out.data_ptr() + 2), dict(q_len=t.data_ptr() + 1)):
         assert call(**kw) == binding.ERR_INVALID_ARG, kw
         assert b"prefill_attention" in lib.uncomp_last_error(ctx.handle)
-    for kw in (dict(dtype=2), dict(D=96), dict(D=256), dict(q_rows=1 << 30), dict(n_seq=(1 << 16) + 1), dict(H=1 << 21)):
+    for kw in (dict(dtype=2), dict(D=96), dict(D=256), dict(q_rows=1 << 30), dict(n_seq=(1 << 16) + 1), dict(H=1 << 21), dict(H=1 << 14, G=1, q_rows=1 << 18)):
         assert call(**kw) == binding.ERR_UNSUPPORTED, kw
     torch.cuda.synchronize()
     assert (out == 3.0).all()

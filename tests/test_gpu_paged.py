@@ -551,7 +551,7 @@ def test_refusals(ctx):
         for kw in (dict(K_pages=None), dict(V_pages=None), dict(idx_pages=None), dict(cum_pages=None), dict(table=None), dict(len=None),
                    dict(n_heads=0), dict(n_pages=0), dict(max_pages=-1), dict(K_pages=c.K.data_ptr() + 8), dict(len=c.length.data_ptr() + 1)):
             assert f(cache(**kw)) == binding.ERR_INVALID_ARG, kw
-        for kw in (dict(dtype=2), dict(D=96), dict(page=48), dict(page=8), dict(page=512), dict(max_pages=1 << 23)):
+        for kw in (dict(dtype=2), dict(D=96), dict(page=48), dict(page=8), dict(page=512), dict(max_pages=1 << 23), dict(n_heads=1 << 22)):
             assert f(cache(**kw)) == binding.ERR_UNSUPPORTED, kw
         assert b"paged" in lib.uncomp_last_error(h)
     ok = cache()
