@@ -764,11 +764,11 @@ __device__ Cut last_of_smallest(F&& each, int want, int* hist, int* buf, uint32_
 }  // namespace
 
 // Short heads (at most 64 R rows): a wave per head with every row's key in a register; nobody waits for anybody.  Whole evictions, us: 5120 heads
-// of 720 rows, an eighth of them without weight, 150 (274 with the cut found bit by bit, by counts of the keys below it).  By a wave and by
-// a workgroup per head: 8 heads of 1900 rows 46 / 29, 256 heads 62 / 48, 2000 heads 116 / 202.
-// Where tables of many heads have room for more, the short heads are seen to first (5120 heads of 700 rows, room for 8192, 150; all by workgroups 259).
+// of 1016 rows, 6 % leaving, 132 (274 with the cut found bit by bit, by counts of the keys below it).  By a wave and by
+// a workgroup per head: 8 heads of 1900 rows 46 / 29, 256 heads 62 / 48, 2000 heads 118 / 202.
+// Where tables of many heads have room for more, the short heads are seen to first (5120 heads of 700 rows, room for 8192, 119; all by workgroups 259).
 template <int R, bool POOL>
-__global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos,
+__global__ __launch_bounds__(256, R <= 16 ? 4 : 5) void paged_select_wave_kernel(PagedCache c, const int32_t* __restrict__ budget, const int32_t* __restrict__ pos,
                                                                 int w, PagedEvictPlan p, char* ws, int32_t* __restrict__ evicted) {
     __shared__ __align__(16) int hist_s[4][256];
     const int lane = threadIdx.x & 63, wg = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
@@ -781,27 +781,29 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
     const int in_page = (1 << c.shift) - 1;
     int drop = 0, gaps = 0;
     if (over > 0) {
-        int at[R];                                                        // rows of the pool
         uint32_t key[R];
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int r = 64 * i + lane;
-            at[i] = table[min(r >> c.shift, c.max_pages - 1)];
-        }
+        const auto place_of = [&](int r) { return c.idx[pool_row(c, h, r)]; };
         int may = 0;
         unsigned long long lacking = 0;
 #pragma unroll
+        for (int i = 0; i < R; ++i) key[i] = table[min((64 * i + lane) >> c.shift, c.max_pages - 1)];
+#pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int r = 64 * i + lane;
-            const bool there = r < n && page_ok(c, at[i]);
+            const int r = 64 * i + lane, id = (int)key[i];
+            const bool there = r < n && page_ok(c, id);
             lacking |= __ballot(r < n && !there);
-            at[i] = there ? (at[i] << c.shift) + (r & in_page) : 0;
-            const float f = c.cum[at[i]];
-            key[i] = c.idx[at[i]] <= newest ? weight_key(f) : kStays;
+            const int at = there ? (id << c.shift) + (r & in_page) : 0;
+            const float f = c.cum[at];
+            key[i] = c.idx[at] <= newest ? weight_key(f) : kStays;
             key[i] = there ? key[i] : kStays;
             may += __builtin_popcountll(__ballot(key[i] != kStays));
+            if (R > 16 && i % (R / 2) == R / 2 - 1) __builtin_amdgcn_sched_barrier(0);
         }
         drop = lacking != 0 ? 0 : min(over, may);
+        // (many rows: their numbers are made anew, or those above and the addresses from them would stay in registers all the way, which then hold
+        // three waves in the place of five: 5120 heads of 1016 rows 146 us, not 132)
+        int late = lane;
+        if constexpr (R > 16) asm volatile("" : "+v"(late));
         uint32_t leaves = 0;                                              // bit i: row 64 i + lane
         if (drop > 0) {
             int* hist = hist_s[threadIdx.x >> 6];
@@ -816,7 +818,7 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
                 // of the rows with the last key the lowest positions, of those at the last position the first rows
                 uint32_t place[R];
 #pragma unroll
-                for (int i = 0; i < R; ++i) place[i] = key[i] == cut.key ? position_key(c.idx[at[i]]) : 0u;
+                for (int i = 0; i < R; ++i) place[i] = key[i] == cut.key ? position_key(place_of(64 * i + late)) : 0u;
                 Cut last = last_of_smallest_wave([&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
                     for (int i = 0; i < R; ++i)
@@ -833,15 +835,17 @@ __global__ __launch_bounds__(256) void paged_select_wave_kernel(PagedCache c, co
         }
         const int stay = n - drop;
         int movers = 0;
+        if constexpr (R > 16) asm volatile("" : "+v"(late));
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int r = 64 * i + lane;
+            const int r = 64 * i + late;
             const bool out = leaves >> i & 1, gap = out && r < stay, mover = !out && r >= stay && r < n;
             const unsigned long long g = __ballot(gap), m = __ballot(mover), lower = (1ull << lane) - 1;
-            if (gap) pairs[row_entry<POOL>(c, h, gaps + __builtin_popcountll(g & lower))].x = at[i];
-            if (mover) pairs[row_entry<POOL>(c, h, movers + __builtin_popcountll(m & lower))].y = at[i];
+            if (gap) pairs[row_entry<POOL>(c, h, gaps + __builtin_popcountll(g & lower))].x = (int)pool_row(c, h, r);
+            if (mover) pairs[row_entry<POOL>(c, h, movers + __builtin_popcountll(m & lower))].y = (int)pool_row(c, h, r);
             gaps += __builtin_popcountll(g);
             movers += __builtin_popcountll(m);
+            if (R > 16) __builtin_amdgcn_sched_barrier(0);
         }
         if (lane == 0 && drop > 0) c.len[h] = stay;
     }
