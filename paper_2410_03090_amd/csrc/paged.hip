@@ -175,15 +175,17 @@ __device__ __forceinline__ void attend_rows(WaveAttend<T, D>& a, const PagedCach
         block(r0, s);
     }
     if (first >= end) return;
-    Pages p = pages_of(first), next = pages_of(first + step);
+    // behind the last block its own rows are fetched once more, from the caches; nobody reads what they bring
+    const auto after = [&](int r0) __attribute__((always_inline)) { return r0 + step < end ? r0 + step : r0; };
+    Pages p = pages_of(first), next = pages_of(after(first));
     load_keys(p, first);
     __builtin_amdgcn_sched_barrier(0);                                    // in this order: the wait for the keys leaves the values on their way
     load_values(p, first);
     for (int r0 = first; r0 < end; r0 += step) {
         float s[A::kPerLane];
         a.logits(keys, scale2, s);
-        // (behind the last block the loads are those of some page: nobody reads what they bring)
-        load_keys(next, r0 + step);
+        const int r1 = after(r0);
+        load_keys(next, r1);
         if (!p.ok(c, 0) || !p.ok(c, 1))
 #pragma unroll
             for (int e = 0; e < A::kPerLane; ++e)
@@ -192,9 +194,9 @@ __device__ __forceinline__ void attend_rows(WaveAttend<T, D>& a, const PagedCach
                     A::clear_value(values, e);
                 }
         block(r0, s);
-        load_values(next, r0 + step);
+        load_values(next, r1);
         p = next;
-        next = pages_of(r0 + 2 * step);
+        next = pages_of(after(r1));
     }
 }
 
