@@ -136,8 +136,8 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
 
 size_t uncomp_paged_workspace_bytes(int n_heads, int G, int D, int rows) {
     if (n_heads <= 0 || G <= 0 || D <= 0 || rows <= 0) return 0;
-    size_t need = paged_append_bytes(n_heads);
-    const size_t step = plan_paged_step(n_heads, G, D, rows, kNoPool).bytes, evict = plan_paged_evict(n_heads, rows, kNoPool).bytes;
+    size_t need = paged_append_bytes(n_heads);                           // (the step of floats needs workspace wherever that of bf16 does)
+    const size_t step = plan_paged_step(true, n_heads, G, D, rows, kNoPool).bytes, evict = plan_paged_evict(n_heads, rows, kNoPool).bytes;
     need = need > step ? need : step;
     return need > evict ? need : evict;
 }
@@ -181,7 +181,7 @@ uncomp_status uncomp_paged_step(uncomp_ctx* ctx, const uncomp_paged_cache* cache
     if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned4(pos) || !aligned4(out))
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: 16-byte aligned q, k_new and v_new required", who);
     const int rows = c.max_pages << c.shift;
-    const PagedStepPlan p = plan_paged_step(c.n_heads, G, cache->D, rows, (int64_t)c.n_pages << c.shift);
+    const PagedStepPlan p = plan_paged_step(cache->dtype == UNCOMP_F32, c.n_heads, G, cache->D, rows, (int64_t)c.n_pages << c.shift);
     st = take_workspace(ctx, who, p.bytes, stream);
     if (st != UNCOMP_OK) return st;
     OnDevice on(ctx->device);

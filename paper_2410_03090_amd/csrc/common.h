@@ -272,7 +272,7 @@ struct PagedCache {
 };
 // Arrays in the workspace with an entry for every row of every head have as many as the tables have room for, head behind head; or, where
 // that is more than twice the rows of the pool (by_pool), one for each of those.  By the tables / by the pool, us: steps of 8 heads of 128K rows
-// 127 / 131, of 256 heads of 16K 479 / 481; a half of them evicted 242 / 291 and 86 / 99.
+// 126 / 129, of 256 heads of 16K 470 / 477; a half of them evicted 241 / 290 and 85 / 99.
 struct PagedStepPlan {
     int head_rows;       // > 0: a workgroup for each head of fewer rows
     bool split;          // the other heads in parts
@@ -286,7 +286,7 @@ struct PagedStepPlan {
     size_t logit_off;    // float [n_heads][query heads, rounded up to 4, 8 or 16][rows], or [n_pages][query heads, as much][page]
     size_t bytes;
 };
-PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows, int64_t pool_rows);
+PagedStepPlan plan_paged_step(bool f32, int n_heads, int G, int D, int rows, int64_t pool_rows);
 struct PagedEvictPlan {
     int rows;
     bool by_pool;

@@ -12,16 +12,23 @@ namespace uncomp {
 namespace {
 
 constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / 64;
-constexpr int kFinishThreads = 256, kFinishRows = 1024, kFinishWgs = 8192;      // kFinishWgs: about the most workgroups for rows, whatever room the tables have
+constexpr int kFinishThreads = 256, kFinishRows = 1024;
+constexpr int kFinishWgs = 8192;                      // about the most workgroups for rows, whatever room the tables have
 constexpr int kSplitAim = 768;                        // workgroups of the attention of few heads: three a CU
 constexpr int kLeastShare = 128;                      // rows of a workgroup, at least: a block a wave
-// One workgroup a head: from as many heads on as fill the chip, with logits that leave room for two workgroups on a CU.  Where tables have room
-// for more rows than that, for the heads that hold few enough for three; the rest in parts.  All heads in parts / so, us, heads of G 4 with tables
-// for 8192 and 20480 rows: 600 of 350 - 700 rows 77 / 47, 5120 of them 674 / 326, 600 of 1500 - 3000 189 / 167, 600 of 3000 - 6000 (a few of
-// them short) 340 / 420, 600 of 10000 - 20000 1046 / 1062.
-constexpr int kHeadLaunchHeads = 512;
+// One workgroup a head, with logits that leave room for two workgroups on a CU, takes about 8 us and 1 more for every 125 rows, whatever the
+// number of heads; parts of heads and their join 12 and 1 for every 15500 rows of all heads.  One workgroup / parts, us, heads of G 4, tables
+// full to three quarters on the average: 8 heads of 300 rows 8.4 / 11.9, of 700 11.1 / 11.9, of 1016 13.6 / 12.0, of 2736 29 / 13; 48 of 1016
+// 14.2 / 15.0; 110 of 2736 31.4 / 30.9; 256 of 300 9.8 / 19.1, of 2736 49 / 57; 500 of 2736 109 / 136.  A row of floats takes twice as long: 48
+// heads of 700 21.9 / 16.6, 256 of 1000 37.8 / 46.3.
+constexpr int kHeadsWorth = 124, kRowsWorth = 80000;
+// Where tables of many heads have room for more rows than LDS, the heads that hold few enough for three workgroups take the one form and the rest
+// the other.  All heads in parts / so, us, heads of G 4 with tables for 8192 and 20480 rows: 600 of 350 - 700 rows 72 / 45, 5120 of them
+// 641 / 293, 600 of 1500 - 3000 181 / 165, 600 of 3000 - 6000 (a few of them short) 327 / 415, 600 of 10000 - 20000 1012 / 1042.
+constexpr int kManyHeads = 512;
 constexpr size_t kHeadLaunchLds = 76 * 1024, kShortHeadLds = 50 * 1024;
-constexpr int kSelectThreads = 1024, kSelectKeys = 32768, kWaveSelectHeads = 512, kWaveSelectRows = 32;      // threads of a selection, keys that it holds in LDS; a wave's most rows a lane
+constexpr int kSelectThreads = 1024, kSelectKeys = 32768;                        // threads of a selection, keys that it holds in LDS
+constexpr int kWaveSelectHeads = 512, kWaveSelectRows = 32;                      // heads from which a wave takes more rows, its most a lane
 
 __device__ __forceinline__ int head_rows(const PagedCache& c, int h) {
     const int cap = c.max_pages << c.shift;
@@ -256,7 +263,8 @@ struct RowLogits {
 }  // namespace
 
 // GT: bound on the query heads per KV head.
-// Many heads: one workgroup per head does all of the step (some: if it has fewer than `stride` rows).  The logits stay in LDS until the sums are known; then every row's weights go to
+// Many heads, or short ones: one workgroup per head does all of the step (some: if it has fewer than `stride` rows).  The logits stay in LDS until
+// the sums are known; then every row's weights go to
 // its cum, and the waves' outputs are joined in the same LDS.
 template <typename T, int D, int GT>
 __global__ __launch_bounds__(kAttendThreads, 3) void paged_head_kernel(PagedCache c, const T* __restrict__ q, const T* __restrict__ k_new,
@@ -374,7 +382,7 @@ __global__ __launch_bounds__(1024) void paged_list_kernel(PagedCache c, int leas
     }
 }
 
-// The rows of few heads, or of the listed ones, are dealt to about as many workgroups as run at a time, whatever the heads' lengths: as many parts
+// The rows of few long heads, or of the listed ones, are dealt to about as many workgroups as run at a time, whatever the heads' lengths: as many parts
 // of a head as it has shares of all rows, begun ones included, and all of one size.  Part number -> head and part of it, from the
 // lengths, 64 of them at a time.
 struct HeadPart {
@@ -1023,18 +1031,19 @@ size_t head_step_lds(int G, int D, int rows) {
 }
 }  // namespace
 
-PagedStepPlan plan_paged_step(int n_heads, int G, int D, int rows, int64_t pool_rows) {
+PagedStepPlan plan_paged_step(bool f32, int n_heads, int G, int D, int rows, int64_t pool_rows) {
     PagedStepPlan p{};
     p.rows = (rows + 31) / 32 * 32;                                       // whole blocks are written
-    if (n_heads >= kHeadLaunchHeads) {
-        p.split = head_step_lds(G, D, p.rows) > kHeadLaunchLds;
+    const bool fits = head_step_lds(G, D, p.rows) <= kHeadLaunchLds;
+    if (n_heads >= kManyHeads || (fits && (int64_t)p.rows * (f32 ? 2 : 1) * (kHeadsWorth - n_heads) <= kRowsWorth)) {
+        p.split = !fits;
         p.head_rows = p.split ? (int)(kShortHeadLds / (heads_bound(G) * sizeof(float))) / 32 * 32 : p.rows;
         if (!p.split) return p;
     }
     p.split = true;
     const int64_t units = (int64_t)n_heads * ((rows + kLeastShare - 1) / kLeastShare);
     // broken parts count half: together about as many as run at a time; of more heads than that, several rounds
-    const int aim = n_heads < kHeadLaunchHeads ? kSplitAim - n_heads / 2 : 4 * kSplitAim;
+    const int aim = n_heads < kManyHeads ? kSplitAim - n_heads / 2 : 4 * kSplitAim;
     p.n_split = (int)(units < aim ? units : aim);
     const size_t parts = (size_t)p.n_split + n_heads;                     // every head may end with a broken one
     size_t off = 0;

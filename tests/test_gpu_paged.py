@@ -122,9 +122,9 @@ def test_long_caches_of_few_heads(ctx, dtype, lens, page):
         _check_step(before[h], _rows(c, h), q[h], kn[h], vn[h], 10 ** 6, out[h].cpu(), dtype, f"head {h}")
 
 
-@pytest.mark.parametrize("heads,lens_to,G", [(1300, 200, 4), (600, 700, 8), (300, 60, 16), (260, 2500, 2)])
+@pytest.mark.parametrize("heads,lens_to,G", [(1300, 200, 4), (600, 700, 8), (300, 60, 16), (260, 2500, 2), (300, 1500, 16), (30, 1500, 4), (150, 1100, 8), (5, 300, 3)])
 def test_many_heads(ctx, heads, lens_to, G):
-    """One workgroup a head and more; every seventh head is checked."""
+    """One workgroup a head, or several; every seventh head is checked."""
     dtype, D, page = torch.bfloat16, 128, 32
     g = torch.Generator().manual_seed(heads)
     lens = torch.randint(0, lens_to + 1, (heads,), generator=g).tolist()
