@@ -414,10 +414,11 @@ uncomp_status uncomp_budgets_from_labels(uncomp_ctx* ctx, const int32_t* labels,
  *   q_first NULL: rows 0 ... q_len[s] - 1, or all q_rows without q_len            (padded)
  *   q_first, q_len NULL: rows q_first[s] ... q_first[s + 1] - 1, n_seq + 1 entries  (packed)
  *   both: q_len[s] rows from q_first[s] on.
- * k_first / k_len say the same of K and V, independently of the queries.  Packed rows usually
- * have a sequence stride of 0.  q_rows / k_rows are the rows that a sequence may address: starts
- * and lengths are cut to them.  Rows of out / lse_out that belong to no sequence are left alone; key
- * rows may be shared by sequences, query rows may not.
+ * k_first / k_len say the same of K and V, independently of the queries.  Packed rows have a sequence
+ * stride of 0; with another one, starts count from the sequence's own rows (a left-padded batch).
+ * q_rows / k_rows are the rows that a sequence may address: starts and lengths are cut to them.
+ * Rows of out / lse_out that belong to no sequence are left alone; key rows may be shared by
+ * sequences, query rows may not.
  * Strides are multiples of 8 elements, none negative, row strides >= D; Q, K, V and out 16-byte aligned;
  * row strides of K and V below 2^24 elements; D 64 or 128; q_rows*G and k_rows <= 2^30; n_seq <= 65536;
  * up to 2^29 query rows times query heads in all.

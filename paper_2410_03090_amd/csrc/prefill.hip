@@ -656,8 +656,9 @@ Plan plan(int tile, bool packed, int n_seq, int H, int G, int D, int q_rows, int
     return p;
 }
 Plan plan(const PrefillArgs& a, bool f32, int D) {
-    const bool packed = a.q.first != nullptr;
-    return plan(tile_of(f32, packed, a.k.first != nullptr, a.n_seq, a.H, a.G, D, a.q.rows, a.k.rows), packed, a.n_seq, a.H, a.G, D, a.q.rows, a.k.rows);
+    // starts alone do not make sequences share the rows: with a stride between them each may have all of q_rows (left-padded batches)
+    const bool packed = a.q.first != nullptr && a.q.ss == 0 && a.o.ss == 0, k_packed = a.k.first != nullptr && a.k.ss == 0 && a.v.ss == 0;
+    return plan(tile_of(f32, packed, k_packed, a.n_seq, a.H, a.G, D, a.q.rows, a.k.rows), packed, a.n_seq, a.H, a.G, D, a.q.rows, a.k.rows);
 }
 }  // namespace
 

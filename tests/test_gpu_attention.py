@@ -314,3 +314,41 @@ def test_refusals(ctx):
     assert (out == 3.0).all()
     assert call() == binding.OK
     torch.cuda.synchronize()
+
+
+def _call_c(ctx, Q, K, V, G, out, lse, **rows):
+    """The C call: Q [n_seq, H*G, q_rows, D], K, V [n_seq, H, k_rows, D], out like Q, lse [n_seq, H*G, q_rows]; rows: q_first, q_len, k_first, k_len."""
+    from paper_2410_03090_amd import binding
+    c3, c2 = binding.ctypes.c_int64 * 3, binding.ctypes.c_int64 * 2
+    n_seq, _, q_rows, D = Q.shape
+    at = {n: torch.tensor(v, dtype=torch.int32, device=DEV) for n, v in rows.items()}
+    p = lambda n: at[n].data_ptr() if n in at else None  # noqa: E731
+    st = binding.load_library().uncomp_prefill_attention(
+        ctx.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), binding.BF16 if Q.dtype == torch.bfloat16 else binding.F32, n_seq, K.shape[1], G, D,
+        q_rows, K.shape[2], p("q_first"), p("q_len"), p("k_first"), p("k_len"), c3(*Q.stride()[:3]), c3(*K.stride()[:3]), c3(*V.stride()[:3]),
+        out.data_ptr(), c3(*out.stride()[:3]), lse.data_ptr(), c2(*lse.stride()[:2]), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return st
+
+
+@pytest.mark.parametrize("n_seq,rows,least,H,G,D,dtype", [(4, 1000, 700, 2, 4, 128, torch.bfloat16), (3, 300, 150, 1, 4, 64, torch.float32),
+                                                         (70, 100, 40, 1, 4, 64, torch.bfloat16), (66, 90, 20, 1, 3, 128, torch.float32)])
+def test_left_padded_batches(ctx, n_seq, rows, least, H, G, D, dtype):
+    """Starts and lengths in a padded batch: every sequence has rows of its own, which end with the batch's last row."""
+    g = torch.Generator().manual_seed(n_seq)
+    n = [rows] + torch.randint(least, rows + 1, (n_seq - 1,), generator=g).tolist()
+    extra = 50
+    Q = torch.randn(n_seq, H * G, rows, D, generator=g).to(dtype)
+    K, V = (torch.randn(n_seq, H, rows + extra, D, generator=g).to(dtype) for _ in range(2))
+    k_len = [m + s % (extra + 1) for s, m in enumerate(n)]
+    out = torch.full(Q.shape, 7.0, dtype=dtype, device=DEV)
+    lse = torch.full(Q.shape[:-1], 7.0, device=DEV)
+    assert _call_c(ctx, Q.to(DEV), K.to(DEV), V.to(DEV), G, out, lse, q_first=[rows - m for m in n], q_len=n,
+                   k_first=[rows + extra - m for m in k_len], k_len=k_len) == 0
+    out, lse = out.cpu(), lse.cpu()
+    for s, m in enumerate(n):
+        a, b = slice(rows - m, rows), slice(rows + extra - k_len[s], rows + extra)
+        assert (out[s, :, :rows - m] == 7.0).all() and (lse[s, :, :rows - m] == 7.0).all()
+        assert (lse[s, :, a] != 7.0).all(), f"sequence {s}: rows without a result"
+        for h in (0, H * G - 1) if n_seq < 10 else (s % (H * G),):
+            _check(Q[s, h, a], K[s, h // G, b], V[s, h // G, b], out[s, h, a], lse[s, h, a], dtype, f"sequence {s}, head {h}")
