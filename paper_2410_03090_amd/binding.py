@@ -43,7 +43,8 @@ class _PagedCacheStruct(ctypes.Structure):
 
 class PagedCache:
     """Rows of every KV head in pages of one pool.  The tensors are updated in place by the paged calls and may be written to by the
-    caller; checked once, here, they stay where they are for the life of the object.
+    caller; checked once, here, they stay where they are for the life of the object, whose attributes cannot be exchanged (the calls pass on
+    the addresses taken here): a cache that has grown is another PagedCache.
 
     K, V [n_pages, page, D]; idx [n_pages, page] int32: original positions; cum [n_pages, page] float32: cumulative scores;
     table [n_heads, max_pages] int32: page numbers, anything outside the pool for no page; length [n_heads] int32: rows in use."""
@@ -57,11 +58,18 @@ class PagedCache:
         assert idx.dtype == table.dtype == length.dtype == torch.int32 and cum.dtype == torch.float32 and length.shape == (n_heads,)
         for t in (K, V, idx, cum, table, length):
             assert t.is_contiguous() and t.is_cuda and t.device == K.device
-        self.K, self.V, self.idx, self.cum, self.table, self.length = K, V, idx, cum, table, length
-        self.n_heads, self.D, self.dtype, self.device = n_heads, D, K.dtype, K.device
-        self._struct = _PagedCacheStruct(K.data_ptr(), V.data_ptr(), idx.data_ptr(), cum.data_ptr(), table.data_ptr(), length.data_ptr(),
-                                         _dtype_code(K), n_heads, n_pages, page, max_pages, D)
-        self._ref = ctypes.byref(self._struct)
+        struct = _PagedCacheStruct(K.data_ptr(), V.data_ptr(), idx.data_ptr(), cum.data_ptr(), table.data_ptr(), length.data_ptr(),
+                                   _dtype_code(K), n_heads, n_pages, page, max_pages, D)
+        for name, value in zip(self.__slots__, (K, V, idx, cum, table, length, n_heads, D, K.dtype, K.device, struct, ctypes.byref(struct))):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        # (cache.length += 1 gives the same tensor its name again)
+        if name not in self.__slots__ or value is not getattr(self, name):
+            raise AttributeError(f"{name} of a paged cache cannot be exchanged: write into it, or make another PagedCache")
+
+    def __delattr__(self, name):
+        raise AttributeError(f"{name} of a paged cache cannot be removed")
 
     def __iter__(self):
         return iter((self.K, self.V, self.idx, self.cum, self.table, self.length))
