@@ -5,7 +5,8 @@ using namespace uncomp;
 
 namespace {
 
-// The context's device is current while a call launches, whatever the caller's is.
+// The context's device is current while a call launches, whatever the caller's is, and before it makes the caller's stream wait for the
+// side stream: the default stream (NULL) is the current device's.
 class OnDevice {
 public:
     explicit OnDevice(int device) {
@@ -38,6 +39,7 @@ constexpr int64_t kMostThreads = 0xffffffffLL;      // of a launch, in all
 constexpr int64_t kMostColumns = 1 << 30, kNoPool = INT64_MAX / 4;
 
 // The workspace starts at offset 0: scores' key ranges are overwritten, side-stream work of an earlier call may still use it.
+// (With the context's device current.)
 uncomp_status take_workspace(uncomp_ctx* ctx, const char* who, size_t need, void* stream) {
     if (need > ctx->ws_bytes)
         return fail(ctx, UNCOMP_ERR_WORKSPACE, "%s: needs %zu workspace bytes, context has %zu", who, need, ctx->ws_bytes);
@@ -122,13 +124,13 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
         a.lse_sh = lse_strides[1];
     }
     if (!prefill_attention_fits(a, dtype, D)) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
+    OnDevice on(ctx->device);
+    if (on.err != hipSuccess) return hip_fail(ctx, on.err, who);
     // (beyond that, what the call leaves in the workspace is as much as fits there)
     uncomp_status st = take_workspace(ctx, who, prefill_attention_least_bytes(n_seq), stream);
     if (st != UNCOMP_OK) return st;
     st = take_workspace(ctx, who, ctx->ws_bytes, stream);
     if (st != UNCOMP_OK) return st;
-    OnDevice on(ctx->device);
-    if (on.err != hipSuccess) return hip_fail(ctx, on.err, who);
     hipError_t e = launch_prefill_attention(a, dtype, D, ctx->ws, ctx->ws_bytes, Env{static_cast<hipStream_t>(stream), &ctx->prof, ctx->force_alu});
     if (e != hipSuccess) return hip_fail(ctx, e, "prefill_attention: launch");
     return UNCOMP_OK;
@@ -156,10 +158,10 @@ uncomp_status uncomp_paged_append(uncomp_ctx* ctx, const uncomp_paged_cache* cac
     if (!aligned16(K) || !aligned16(V) || !aligned4(idx) || !aligned4(cum) || !aligned4(n_rows))
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: 16-byte aligned K and V required", who);
     if ((int64_t)c.n_heads * (((int64_t)rows + 63) / 64) * 256 > kMostThreads) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
-    st = take_workspace(ctx, who, paged_append_bytes(c.n_heads), stream);
-    if (st != UNCOMP_OK) return st;
     OnDevice on(ctx->device);
     if (on.err != hipSuccess) return hip_fail(ctx, on.err, who);
+    st = take_workspace(ctx, who, paged_append_bytes(c.n_heads), stream);
+    if (st != UNCOMP_OK) return st;
     const int row_size = row_bytes_of(cache), elem = row_size / cache->D;
     hipError_t e = launch_paged_append(c, K, V, idx, cum, n_rows, rows, strides[0] * elem, strides[1] * elem, row_size, ctx->ws,
                                        Env{static_cast<hipStream_t>(stream), &ctx->prof, ctx->force_alu});
@@ -182,10 +184,10 @@ uncomp_status uncomp_paged_step(uncomp_ctx* ctx, const uncomp_paged_cache* cache
         return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: 16-byte aligned q, k_new and v_new required", who);
     const int rows = c.max_pages << c.shift;
     const PagedStepPlan p = plan_paged_step(cache->dtype == UNCOMP_F32, c.n_heads, G, cache->D, rows, (int64_t)c.n_pages << c.shift);
-    st = take_workspace(ctx, who, p.bytes, stream);
-    if (st != UNCOMP_OK) return st;
     OnDevice on(ctx->device);
     if (on.err != hipSuccess) return hip_fail(ctx, on.err, who);
+    st = take_workspace(ctx, who, p.bytes, stream);
+    if (st != UNCOMP_OK) return st;
     hipError_t e = launch_paged_step(c, q, k_new, v_new, cache->dtype, pos, G, cache->D, p, ctx->ws, out,
                                      Env{static_cast<hipStream_t>(stream), &ctx->prof, ctx->force_alu});
     if (e != hipSuccess) return hip_fail(ctx, e, "paged_step: launch");
@@ -203,10 +205,10 @@ uncomp_status uncomp_paged_evict(uncomp_ctx* ctx, const uncomp_paged_cache* cach
     if (w < 0) return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: w must not be negative", who);
     if (!aligned4(budget) || !aligned4(pos) || !aligned4(evicted)) return fail(ctx, UNCOMP_ERR_INVALID_ARG, "%s: misaligned pointer", who);
     const PagedEvictPlan p = plan_paged_evict(c.n_heads, c.max_pages << c.shift, (int64_t)c.n_pages << c.shift);
-    st = take_workspace(ctx, who, p.bytes, stream);
-    if (st != UNCOMP_OK) return st;
     OnDevice on(ctx->device);
     if (on.err != hipSuccess) return hip_fail(ctx, on.err, who);
+    st = take_workspace(ctx, who, p.bytes, stream);
+    if (st != UNCOMP_OK) return st;
     hipError_t e = launch_paged_evict(c, budget, pos, w, row_bytes_of(cache), p, ctx->ws, evicted,
                                       Env{static_cast<hipStream_t>(stream), &ctx->prof, ctx->force_alu});
     if (e != hipSuccess) return hip_fail(ctx, e, "paged_evict: launch");
