@@ -134,8 +134,9 @@ uncomp_status uncomp_measure_peaks(uncomp_ctx* ctx, const void* buf, size_t byte
  * stream.  The workspace must hold the entropy and scoring regions side by side, which is
  * what uncomp_workspace_bytes reports.  Every other call that touches the workspace regions
  * of the side-stream work (a second uncomp_head_entropy, uncomp_decode_step,
- * uncomp_hidden_evict, uncomp_matrix_entropy, uncomp_prepare_accumulate) joins first by
- * itself, so calls may follow one another in any order. */
+ * uncomp_hidden_evict, uncomp_matrix_entropy, uncomp_prepare_accumulate; uncomp_prefill_attention
+ * and the paged calls where they take workspace) joins first by itself, so calls may follow one
+ * another in any order. */
 uncomp_status uncomp_set_overlap(uncomp_ctx* ctx, int on);
 uncomp_status uncomp_join(uncomp_ctx* ctx, void* stream);
 

@@ -126,10 +126,7 @@ uncomp_status uncomp_prefill_attention(uncomp_ctx* ctx, const void* Q, const voi
     if (!prefill_attention_fits(a, dtype, D)) return fail(ctx, UNCOMP_ERR_UNSUPPORTED, "%s: problem too large", who);
     OnDevice on(ctx->device);
     if (on.err != hipSuccess) return hip_fail(ctx, on.err, who);
-    // (beyond that, what the call leaves in the workspace is as much as fits there)
-    uncomp_status st = take_workspace(ctx, who, prefill_attention_least_bytes(n_seq), stream);
-    if (st != UNCOMP_OK) return st;
-    st = take_workspace(ctx, who, ctx->ws_bytes, stream);
+    uncomp_status st = take_workspace(ctx, who, prefill_attention_takes(a, dtype, D, ctx->ws_bytes), stream);
     if (st != UNCOMP_OK) return st;
     hipError_t e = launch_prefill_attention(a, dtype, D, ctx->ws, ctx->ws_bytes, Env{static_cast<hipStream_t>(stream), &ctx->prof, ctx->force_alu});
     if (e != hipSuccess) return hip_fail(ctx, e, "prefill_attention: launch");

@@ -329,7 +329,7 @@ struct PrefillArgs {
     int64_t* sums;       // tiles of the sequences up to each, where there are many
 };
 bool prefill_attention_fits(const PrefillArgs& a, uncomp_dtype dt, int D);       // the launch's grid
-size_t prefill_attention_least_bytes(int n_seq);                                 // without which it does not run
+size_t prefill_attention_takes(const PrefillArgs& a, uncomp_dtype dt, int D, size_t ws_bytes);       // of a workspace of ws_bytes (more: does not run)
 size_t prefill_attention_bytes(int n_seq, int H, int G, int D, int q_rows, int k_rows);
 hipError_t launch_prefill_attention(const PrefillArgs& a, uncomp_dtype dt, int D, char* ws, size_t ws_bytes, const Env& env);
 

@@ -673,7 +673,10 @@ size_t prefill_attention_bytes(int n_seq, int H, int G, int D, int q_rows, int k
 }
 
 bool prefill_attention_fits(const PrefillArgs& a, uncomp_dtype dt, int D) { return plan(a, dt == UNCOMP_F32, D).items * 512 <= 0xffffffffLL; }
-size_t prefill_attention_least_bytes(int n_seq) { return n_seq > kRanked ? (size_t)n_seq * sizeof(int64_t) : 0; }
+size_t prefill_attention_takes(const PrefillArgs& a, uncomp_dtype dt, int D, size_t ws_bytes) {
+    const size_t bytes = plan(a, dt == UNCOMP_F32, D).bytes;
+    return a.n_seq > kRanked || bytes <= ws_bytes ? bytes : 0;           // (no room for parts: whole tiles)
+}
 
 namespace {
 template <int D>

@@ -352,3 +352,42 @@ def test_left_padded_batches(ctx, n_seq, rows, least, H, G, D, dtype):
         assert (lse[s, :, a] != 7.0).all(), f"sequence {s}: rows without a result"
         for h in (0, H * G - 1) if n_seq < 10 else (s % (H * G),):
             _check(Q[s, h, a], K[s, h // G, b], V[s, h // G, b], out[s, h, a], lse[s, h, a], dtype, f"sequence {s}, head {h}")
+
+
+def test_a_call_without_workspace_leaves_it_alone():
+    """Attention that takes no workspace does not join the side stream: the entropies' region stays theirs, and scores that do not fit beside it are
+    refused as they are without the attention in between.  With a join, and attention that does take workspace, they fit."""
+    from paper_2410_03090_amd import binding
+    H, G, N, w, D = 8, 4, 8192, 32, 128
+    g = torch.Generator().manual_seed(35)
+    Q = torch.randn(1, H * G, N, D, generator=g).to(torch.bfloat16).to(DEV)
+    K, V = (torch.randn(1, H, N, D, generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
+    win = Q[:, :, N - w:].contiguous()
+    score = binding.Context.workspace_bytes(0, N, D, 1, H, G, w)
+    front = binding.Context.workspace_bytes(0, 0, D, 0, 0, 0, 0)
+    least = front + 2 * H * (128 * 128 * 4 + 128 * 4)                    # two chunks of every matrix, the fewest
+    c = binding.Context(0, max(score, least))
+    assert max(score, least) < score + least - front
+    assert binding.Context.prefill_attention_workspace_bytes(1, H, G, D, N, N) == 0
+    want = c.window_score(win, K, G)
+    ref = c.head_entropy(K.view(H, N, D))
+    att, _ = c.prefill_attention(Q, K, V, G)
+    c.set_overlap(True)
+    ent = c.head_entropy(K.view(H, N, D))
+    got, _ = c.prefill_attention(Q, K, V, G)
+    with pytest.raises(binding.UncompError) as e:
+        c.window_score(win, K, G)
+    assert e.value.status == binding.ERR_WORKSPACE
+    c.join()
+    again = c.window_score(win, K, G)
+    torch.cuda.synchronize()
+    assert torch.equal(ent, ref) and torch.equal(got, att) and torch.equal(again, want)
+    few = [(1, 2)] * 65                                                  # (more than 64 sequences take some)
+    q, k, v, qs, ks = _packed(few, 1, G, D, torch.bfloat16, 36)
+    ent = c.head_entropy(K.view(H, N, D))
+    out, lse = _run_packed(c, q, k, v, G, qs, ks)
+    again = c.window_score(win, K, G)
+    torch.cuda.synchronize()
+    _check_packed(q, k, v, G, qs, ks, out, lse, torch.bfloat16, heads=[0])
+    assert torch.equal(ent, ref) and torch.equal(again, want)
+    c.close()
