@@ -536,16 +536,17 @@ class Context:
         """K / V [n_heads, cap, D] (last dim contiguous), idx [n_heads, cap] int32, cum [n_heads, cap] float32 or None (zeros), rows
         [n_heads] int32 the rows offered of every head (None: all).  cache.length tells what was taken."""
         n_heads, cap, D = K.shape
-        assert K.shape == V.shape and K.stride() == V.stride() and K.stride(2) == 1 and K.dtype == V.dtype == cache.dtype
+        assert K.shape == V.shape and K.stride(2) == V.stride(2) == 1 and K.dtype == V.dtype == cache.dtype
+        strides, v_strides = ((t.stride(0) if n_heads > 1 else 0, t.stride(1) if cap > 1 else D) for t in (K, V))
+        assert strides == v_strides, "K and V of one layout"
         assert n_heads == cache.n_heads and D == cache.D and cache.device.index == self.device
         assert idx.shape == (n_heads, cap) and idx.dtype == torch.int32 and idx.is_contiguous()
         assert cum is None or (cum.shape == (n_heads, cap) and cum.dtype == torch.float32 and cum.is_contiguous())
         assert rows is None or (rows.shape == (n_heads,) and rows.dtype == torch.int32 and rows.is_contiguous())
         for t in (K, V, idx, cum, rows):
             assert t is None or t.device == cache.device
-        strides = _I64x2(K.stride(0) if n_heads > 1 else 0, K.stride(1) if cap > 1 else D)
         self._check(self.lib.uncomp_paged_append(self.handle, cache._ref, K.data_ptr(), V.data_ptr(), idx.data_ptr(), _ptr(cum), _ptr(rows), cap,
-                                                 strides, self._raw_stream()))
+                                                 _I64x2(*strides), self._raw_stream()))
 
     def paged_step(self, cache: PagedCache, q: torch.Tensor, k_new=None, v_new=None, pos=None, out=None, want_out: bool = True):
         """q [n_heads, G, D], k_new / v_new [n_heads, D], pos [n_heads] int32 (the three may be None together).  Returns out

@@ -576,3 +576,30 @@ def test_refusals(ctx):
     small.close()
     for a, b in zip(state, _host(c)):
         assert np.array_equal(a, b)
+
+
+def test_append_strides_of_one_head_or_one_row(ctx):
+    """A dimension of one entry has any stride: K and V need not agree there."""
+    D, cap = 128, 40
+    g = torch.Generator().manual_seed(52)
+    wide = torch.randn(cap, 3 * D, generator=g).to(torch.bfloat16).to(DEV)
+    K = wide[:, :D].unsqueeze(0)
+    V = wide.view(cap, 3, D)[:, 1:2].transpose(0, 1)
+    assert K.stride(0) != V.stride(0) and K.stride(1) == V.stride(1)
+    idx = torch.arange(cap, dtype=torch.int32, device=DEV)[None]
+    c = ctx.paged_new(1, 4, 16, 4, D)
+    c.table.copy_(torch.tensor([[2, 0, 3, 1]], dtype=torch.int32))
+    ctx.paged_append(c, K, V, idx)
+    torch.cuda.synchronize()
+    k, v, i, s = _rows(c, 0)
+    assert len(k) == cap and torch.equal(k, K[0].cpu()) and torch.equal(v, V[0].cpu()) and torch.equal(i, idx[0].cpu()) and (s == 0).all()
+    n = 5
+    K = torch.randn(n, 2, D, generator=g).to(torch.bfloat16).to(DEV)[:, :1]
+    V = torch.randn(n, 2 * D, generator=g).to(torch.bfloat16).to(DEV)[:, :D].as_strided((n, 1, D), (2 * D, 8, 1))
+    c = ctx.paged_new(n, n, 16, 1, D)
+    c.table.copy_(torch.arange(n, dtype=torch.int32).view(n, 1))
+    ctx.paged_append(c, K, V, torch.full((n, 1), 3, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    for h in range(n):
+        k, v, i, _ = _rows(c, h)
+        assert torch.equal(k, K[h].cpu()) and torch.equal(v, V[h].cpu()) and i.tolist() == [3]
