@@ -516,7 +516,7 @@ class Context:
             lse = torch.full(Q.shape[:-1], float("-inf"), dtype=torch.float32, device=Q.device)
         ls = None
         if lse is not None:
-            assert lse.shape == Q.shape[:-1] and lse.dtype == torch.float32 and lse.stride(-1) == 1 and lse.device == Q.device
+            assert lse.shape == Q.shape[:-1] and lse.dtype == torch.float32 and (Nq == 1 or lse.stride(-1) == 1) and lse.device == Q.device
             ls = _I64x2(lse.stride(0) if q_first is None else 0, lse.stride(-2))
         self._check(self.lib.uncomp_prefill_attention(
             self.handle, Q.data_ptr(), K.data_ptr(), V.data_ptr(), _dtype_code(Q), n_seq, H, int(G), D, Nq, Nk, _ptr(q_first), _ptr(q_len),

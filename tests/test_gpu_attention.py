@@ -391,3 +391,16 @@ def test_a_call_without_workspace_leaves_it_alone():
     _check_packed(q, k, v, G, qs, ks, out, lse, torch.bfloat16, heads=[0])
     assert torch.equal(ent, ref) and torch.equal(again, want)
     c.close()
+
+
+def test_normalisers_of_one_row_have_any_row_stride(ctx):
+    B, H, G, D = 3, 2, 2, 128
+    g = torch.Generator().manual_seed(37)
+    Q = torch.randn(B, H * G, 1, D, generator=g).to(torch.bfloat16)
+    K, V = (torch.randn(B, H, 50, D, generator=g).to(torch.bfloat16) for _ in range(2))
+    lse = torch.zeros(1, B, H * G, device=DEV).permute(1, 2, 0)
+    out, _ = ctx.prefill_attention(Q.to(DEV), K.to(DEV), V.to(DEV), G, lse=lse)
+    torch.cuda.synchronize()
+    for b in range(B):
+        for h in range(H * G):
+            _check(Q[b, h], K[b, h // G], V[b, h // G], out[b, h].cpu(), lse[b, h].cpu(), torch.bfloat16, f"batch {b}, head {h}")
