@@ -403,7 +403,8 @@ __device__ __forceinline__ bool find_head_part(const PagedCache& c, const PagedS
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
     }
-    int share = (int)max((int64_t)kLeastShare, min((total + p.n_split - 1) / p.n_split, (int64_t)1 << 26));
+    // (at most one row more than a head can have, which is then one part: never more parts than n_split and a broken one a head)
+    int share = (int)max((int64_t)kLeastShare, min((total + p.n_split - 1) / p.n_split, ((int64_t)1 << 26) + 1));
     if (share < 4 * kLeastShare) share = (share + kLeastShare - 1) / kLeastShare * kLeastShare;      // as many blocks for every wave, where they are few
     for (int h0 = 0; h0 < n_heads; h0 += 64) {
         const int i = min(h0 + lane, n_heads - 1), h = LISTED ? list[1 + i] : i;
