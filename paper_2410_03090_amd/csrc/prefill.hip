@@ -60,7 +60,7 @@ __device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile, int64_
     if (a.n_seq == 1) {                                    // nothing to look for: its last tile sees most
         seq_of(0, &qf, &nq, &kf, &nk);
         const int n = tiles_of(nq), first = max(0, min(nk, nk - nq + (tile - 1) / a.G + 1));
-        *out = Tile{0, n - 1 - (int)rank, qf, nq, kf, nk, (int64_t)n * (first + nk) / 128};
+        *out = Tile{0, n - 1 - (int)rank, qf, nq, kf, nk, n * ((int64_t)first + nk) / 128};
         return rank < n;
     }
     if (a.n_seq <= kRanked) {
@@ -69,7 +69,7 @@ __device__ __forceinline__ bool find_tile(const PrefillArgs& a, int tile, int64_
         if (rank >= wave_total(n)) return false;
         if (a.n_split > 1) {
             const int first = max(0, min(nk, nk - nq + (tile - 1) / a.G + 1));
-            out->blocks = wave_total((int64_t)n * (first + nk) / 128);
+            out->blocks = wave_total(n * ((int64_t)first + nk) / 128);
         }
         int most = (nk + 63) / 64;
 #pragma unroll
