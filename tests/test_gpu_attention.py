@@ -404,3 +404,29 @@ def test_normalisers_of_one_row_have_any_row_stride(ctx):
     for b in range(B):
         for h in range(H * G):
             _check(Q[b, h], K[b, h // G], V[b, h // G], out[b, h].cpu(), lse[b, h].cpu(), torch.bfloat16, f"batch {b}, head {h}")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nq,nk,ws", [(400, 400, 64 << 20), (100, 3000, 64 << 20), (100, 3000, 256)])
+def test_infinite_values_arrive_where_they_are_seen(ctx, dtype, D, nq, nk, ws):
+    """Infinities of both signs and NaN among the values, in tiles that all rows see and in masked ones, in parts of a tile and not: rows before them
+    stay finite, rows from them on have them, both signs together are NaN."""
+    from paper_2410_03090_amd import binding
+    G = 2
+    Q, K, V, qs, ks = _packed([(nq, nk)], 1, G, D, dtype, 31)
+    late = nk - nq                                                       # the first row's last key
+    for key, feature, value in ((late + 90, 3, "inf"), (late + 91, 4, "-inf"), (late + 40, 7, "nan"), (late + 60, 8, "inf"), (late + 65, 8, "-inf"),
+                                (20, 5, "inf"), (21, 6, "-inf"), (nk - 1, 9, "-inf"), (nk - 2, 10, "inf"), (late + 63, 11, "inf"), (late + 64, 12, "-inf")):
+        V[0, key, feature] = float(value)
+    small = binding.Context(0, ws)
+    out, lse = _run_packed(small, Q, K, V, G, qs, ks)
+    small.close()
+    _check_packed(Q, K, V, G, qs, ks, out, lse, dtype)
+    assert lse.isfinite().all()
+    for h in range(G):
+        ref = O.causal_attention(to_f64(Q[h]), to_f64(K[0]), to_f64(V[0]))[0]
+        got = to_f64(out[h])
+        assert np.array_equal(np.isnan(got), np.isnan(ref))
+        odd = ~np.isfinite(ref)
+        assert np.array_equal(~np.isfinite(got), odd) and np.array_equal(got[odd & ~np.isnan(ref)], ref[odd & ~np.isnan(ref)])
