@@ -430,3 +430,16 @@ def test_infinite_values_arrive_where_they_are_seen(ctx, dtype, D, nq, nk, ws):
         assert np.array_equal(np.isnan(got), np.isnan(ref))
         odd = ~np.isfinite(ref)
         assert np.array_equal(~np.isfinite(got), odd) and np.array_equal(got[odd & ~np.isnan(ref)], ref[odd & ~np.isnan(ref)])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("seqs", [[(300, 300), (1, 7)], [(3, 9000)], [(3, 4)] * 70])
+def test_without_normalisers(ctx, dtype, seqs):
+    G, D, H = 4, 128, 1
+    Q, K, V, qs, ks = _packed(seqs, H, G, D, dtype, 32)
+    out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    alone, none = ctx.prefill_attention(Q.to(DEV), K.to(DEV), V.to(DEV), G, q_first=i32(qs), k_first=i32(ks), want_lse=False)
+    torch.cuda.synchronize()
+    assert none is None and torch.equal(alone.cpu(), out)
+    _check_packed(Q, K, V, G, qs, ks, alone.cpu(), lse, dtype, heads=[0, 3])

@@ -603,3 +603,28 @@ def test_append_strides_of_one_head_or_one_row(ctx):
     for h in range(n):
         k, v, i, _ = _rows(c, h)
         assert torch.equal(k, K[h].cpu()) and torch.equal(v, V[h].cpu()) and i.tolist() == [3]
+
+
+@pytest.mark.parametrize("n,lens_to,long,max_pages,G,dtype", [(40, 60, 0, 2, 4, torch.bfloat16), (2, 5, 20011, 314, 4, torch.bfloat16),
+                                                              (3, 9, 9001, 600, 7, torch.float32), (600, 60, 4000, 90, 8, torch.bfloat16),
+                                                              (700, 20, 2000, 700, 16, torch.float32)])
+def test_steps_without_outputs(ctx, n, lens_to, long, max_pages, G, dtype):
+    """One workgroup a head, heads in parts, listed heads, workspace by the tables and by the pool: without outputs the cache becomes what it becomes
+    with them."""
+    D, page = 64, 64
+    lens = [(37 * h) % (lens_to + 1) for h in range(n)]
+    if long:
+        lens[0], lens[n // 2] = long, long - 77
+    pair = [_cache(ctx, lens, page, max_pages, D, dtype, 51, room=2)[0] for _ in range(2)]
+    pick = sorted({0, 1, n // 2, n - 1})
+    for t in range(2):
+        q, kn, vn = _token(n, G, D, dtype, 95 + t)
+        before = {h: _rows(pair[0], h) for h in pick}
+        args = [x.to(DEV) for x in (q, kn, vn)] + [torch.full((n,), 10 ** 6 + t, dtype=torch.int32, device=DEV)]
+        out = ctx.paged_step(pair[0], *args)
+        assert ctx.paged_step(pair[1], *args, want_out=False) is None
+        torch.cuda.synchronize()
+        for a, b in zip(_host(pair[0]), _host(pair[1])):
+            assert np.array_equal(a, b)
+        for h in pick:
+            _check_step(before[h], _rows(pair[1], h), q[h], kn[h], vn[h], 10 ** 6 + t, out[h].cpu(), dtype, f"token {t}, head {h}")
