@@ -443,3 +443,41 @@ def test_without_normalisers(ctx, dtype, seqs):
     torch.cuda.synchronize()
     assert none is None and torch.equal(alone.cpu(), out)
     _check_packed(Q, K, V, G, qs, ks, alone.cpu(), lse, dtype, heads=[0, 3])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("packed", ["queries", "keys"])
+def test_packed_on_one_side_only(ctx, dtype, packed):
+    """Packed queries on a padded batch of keys, and a padded batch of queries on packed keys."""
+    H, G, D = 2, 3, 128
+    nq, nk = [70, 0, 130, 5], [90, 33, 130, 260]
+    g = torch.Generator().manual_seed(33)
+    qs, ks = np.cumsum([0] + nq).tolist(), np.cumsum([0] + nk).tolist()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    if packed == "queries":
+        Q = torch.randn(H * G, qs[-1], D, generator=g).to(dtype)
+        K, V = (torch.randn(4, H, max(nk), D, generator=g).to(dtype) for _ in range(2))
+        out, lse = ctx.prefill_attention(Q.to(DEV), K.to(DEV), V.to(DEV), G, q_first=i32(qs), k_len=i32(nk))
+    else:
+        Q = torch.randn(4, H * G, max(nq), D, generator=g).to(dtype)
+        K, V = (torch.randn(H, ks[-1], D, generator=g).to(dtype) for _ in range(2))
+        out, lse = ctx.prefill_attention(Q.to(DEV), K.to(DEV), V.to(DEV), G, q_len=i32(nq), k_first=i32(ks))
+    torch.cuda.synchronize()
+    out, lse = out.cpu(), lse.cpu()
+    for s in range(4):
+        a, b = slice(qs[s], qs[s + 1]), slice(ks[s], ks[s + 1])
+        for h in range(H * G):
+            if packed == "queries":
+                _check(Q[h, a], K[s, h // G, :nk[s]], V[s, h // G, :nk[s]], out[h, a], lse[h, a], dtype, f"sequence {s}, head {h}")
+            else:
+                m = nq[s]
+                _check(Q[s, h, :m], K[h // G, b], V[h // G, b], out[s, h, :m], lse[s, h, :m], dtype, f"sequence {s}, head {h}")
+                assert (out[s, h, m:] == 0).all() and (lse[s, h, m:] == float("-inf")).all()
+
+
+@pytest.mark.parametrize("dtype,D", [(torch.bfloat16, 128), (torch.bfloat16, 64), (torch.float32, 128)])
+@pytest.mark.parametrize("G", [40, 300])
+def test_more_query_heads_than_a_tile_has_columns(ctx, dtype, D, G):
+    Q, K, V, qs, ks = _packed([(3, 70), (9, 9), (2, 2100)], 1, G, D, dtype, 34)
+    out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
+    _check_packed(Q, K, V, G, qs, ks, out, lse, dtype, heads=[0, 1, G // 2, G - 1])
