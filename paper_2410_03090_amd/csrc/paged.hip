@@ -48,12 +48,6 @@ __device__ __forceinline__ int64_t row_entry(const PagedCache& c, int h, int r) 
     return POOL ? pool_row(c, h, r) : (int64_t)h * (c.max_pages << c.shift) + r;
 }
 
-template <int BYTES>
-__device__ __forceinline__ void copy_bytes(const char* src, char* dst) {
-    if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
-    else *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(src);
-}
-
 }  // namespace
 
 // ---- append ----------------------------------------------------------------------------------------------------------
@@ -95,8 +89,8 @@ __global__ __launch_bounds__(256) void paged_copy_kernel(PagedCache c, const cha
     const int lanes = row_size / 16, per = 256 / lanes, piece = (threadIdx.x % lanes) * 16;
     for (int r = r0 + threadIdx.x / lanes; r < end; r += per) {
         const int64_t to = pool_row(c, h, f.x + r) * row_size + piece, from = h * head_bytes + r * row_bytes + piece;
-        copy_bytes<16>(K + from, reinterpret_cast<char*>(c.K) + to);
-        copy_bytes<16>(V + from, reinterpret_cast<char*>(c.V) + to);
+        *reinterpret_cast<uint4*>(static_cast<char*>(c.K) + to) = *reinterpret_cast<const uint4*>(K + from);
+        *reinterpret_cast<uint4*>(static_cast<char*>(c.V) + to) = *reinterpret_cast<const uint4*>(V + from);
     }
     const int r = r0 + threadIdx.x;
     if (threadIdx.x < 64 && r < end) {
@@ -982,7 +976,8 @@ __global__ __launch_bounds__(kSelectThreads) void paged_select_kernel(PagedCache
              [&](int r) { pairs[row_entry<POOL>(c, h, from++)].y = (int)pool_row(c, h, r); });
 }
 
-// Moves the paired rows: 16 bytes a lane of K and of V, four pairs at a time.
+// Moves the paired rows: 16 bytes a lane of K and of V, four pairs at a time.  (Three of the four pieces of K wait in scratch memory, 48 bytes a lane
+// out and in again: a third of what the kernel writes.)
 template <bool POOL>
 __global__ __launch_bounds__(256) void paged_move_kernel(PagedCache c, int row_size, int n_chunks, PagedEvictPlan p, const char* __restrict__ ws) {
     const int h = spread_head(blockIdx.x / n_chunks, c.n_heads);
