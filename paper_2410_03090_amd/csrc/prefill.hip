@@ -464,6 +464,9 @@ __global__ __launch_bounds__(64 * NW, D == 64 ? 3 : 2) void prefill_tile_kernel(
             m = m_new;
         }
     };
+    // The weights are rounded to bf16, the width of the values that they multiply: half a step is 2^-8 of a weight, as much as the rounding of the result
+    // is of that, and the roundings of many keys mostly cancel.  (Relative error against 64 bits, 8192 rows: 0.0020, of which the result's own rounding
+    // is 0.0016.  Three bf16 a weight, as the paged step has, would double the matrix instructions.)  Their sum is that of the unrounded ones.
     auto weights = [&](const f32x16_t& z, bf16x8_t (&p)[2]) __attribute__((always_inline)) {
         const float ref = reference(m) * scale2;
         float sum[2] = {0.f, 0.f};
@@ -626,8 +629,9 @@ struct Plan {
     int64_t items;       // tiles of all KV heads, at most
     size_t acc_off, bytes;
 };
-// 64-wide heads take tiles of 128 columns, two workgroups a CU: as much work for the vector unit comes with half the products, and
-// two that do not wait for each other fill it better (8 KV heads of 1024 rows 28.5 -> 22.3 us, 8192 rows 357 -> 347).
+// 64-wide heads take tiles of 128 columns, three workgroups a CU: as much work for the vector unit comes with half the products, and
+// several that do not wait for each other fill it better.  8 KV heads of 4 query heads, us, of 8192 rows: one workgroup of 256 columns a CU 357, two of
+// 128 347, three 322 (of 1024 rows 28.5, 22.3 and 23).  Three leave a wave 168 registers: 11 more wait in scratch memory outside the loop.
 // 128-wide ones take tiles of 256, which read keys and values half as often, unless a sequence has not as many columns, or its keys are soon
 // through (what comes before and after them then counts, and another workgroup fills it), or they would not fill the chip.  256 / 128, us, 8
 // KV heads of 4 query heads: 16 sequences of 1 query on 20000 keys 341 / 199, 256 prompts of 128 rows 280 / 248, 32 of 1024 455 / 444, 1 of 1024
