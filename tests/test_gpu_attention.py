@@ -481,3 +481,20 @@ def test_more_query_heads_than_a_tile_has_columns(ctx, dtype, D, G):
     Q, K, V, qs, ks = _packed([(3, 70), (9, 9), (2, 2100)], 1, G, D, dtype, 34)
     out, lse = _run_packed(ctx, Q, K, V, G, qs, ks)
     _check_packed(Q, K, V, G, qs, ks, out, lse, dtype, heads=[0, 1, G // 2, G - 1])
+
+
+@pytest.mark.parametrize("dtype,D", [(torch.bfloat16, 128), (torch.bfloat16, 64), (torch.float32, 128)])
+def test_rows_far_apart(ctx, dtype, D):
+    """The largest row stride of keys and values, and queries and outputs as far apart: offsets within a tile come near 2^31 bytes."""
+    G, nq, nk, stride = 2, 70, 150, (1 << 24) - 8
+    Q, K, V, qs, ks = _packed([(nq, nk)], 1, G, D, dtype, 38)
+    pool = torch.empty((nk - 1) * stride + 4 * D, dtype=dtype, device=DEV)      # K, V and the two query heads side by side; the outputs' in the gaps
+    at = lambda n, heads, first: pool.as_strided((heads, n, D), (D, stride, 1), first)  # noqa: E731
+    k, v, q = at(nk, 1, 0), at(nk, 1, D), at(nq, G, 2 * D)
+    out = pool.as_strided((G, nq, D), (D, stride, 1), 1 << 20)
+    k.copy_(K), v.copy_(V), q.copy_(Q), out.fill_(7.0)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    _, lse = ctx.prefill_attention(q, k, v, G, q_first=i32(qs), k_first=i32(ks), out=out)
+    torch.cuda.synchronize()
+    _check_packed(Q, K, V, G, qs, ks, out.cpu(), lse.cpu(), dtype)
+    assert torch.equal(k.cpu(), K) and torch.equal(v.cpu(), V) and torch.equal(q.cpu(), Q)

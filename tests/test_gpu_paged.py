@@ -628,3 +628,23 @@ def test_steps_without_outputs(ctx, n, lens_to, long, max_pages, G, dtype):
             assert np.array_equal(a, b)
         for h in pick:
             _check_step(before[h], _rows(pair[1], h), q[h], kn[h], vn[h], 10 ** 6 + t, out[h].cpu(), dtype, f"token {t}, head {h}")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_the_smallest_cache(ctx, dtype):
+    """One head with one page of sixteen rows: empty, growing row by row until it is full, cut to one row, cut to none."""
+    G, D = 1, 64
+    c = ctx.paged_new(1, 1, 16, 1, D, dtype)
+    c.table.zero_()
+    for t in range(18):
+        q, kn, vn = _token(1, G, D, dtype, 200 + t)
+        before = _rows(c, 0)
+        out = ctx.paged_step(c, q.to(DEV), kn.to(DEV), vn.to(DEV), torch.full((1,), t, dtype=torch.int32, device=DEV))
+        torch.cuda.synchronize()
+        assert int(c.length[0]) == min(t + 1, 16)
+        _check_step(before, _rows(c, 0), q[0], kn[0] if t < 16 else None, vn[0], t, out[0].cpu(), dtype, f"token {t}")
+    _check_evict(ctx, c, [1], [17], 0)
+    assert int(c.length[0]) == 1
+    _check_evict(ctx, c, [0], [17], 0)
+    assert int(c.length[0]) == 0
+    assert (ctx.paged_step(c, q.to(DEV)) == 0).all() and int(c.length[0]) == 0
