@@ -2,8 +2,10 @@
 // different budgets hold what they need.  Row r of head h is row r % page of page table[h][r / page].
 //
 //   append   rows of dense caches join (paged_reserve_kernel: how many fit; paged_copy_kernel)
-//   step     one new token joins, its queries attend over the rows, weights accumulate (paged_attend_kernel, paged_finish_kernel)
-//   evict    the rows of least accumulated weight leave (paged_select_kernel, paged_move_kernel)
+//   step     one new token joins, its queries attend over the rows, weights accumulate (paged_head_kernel: a head by one workgroup;
+//            paged_attend_kernel, paged_finish_kernel: in parts; paged_list_kernel: which heads, where there are both)
+//   evict    the rows of least accumulated weight leave (paged_select_wave_kernel, paged_select_kernel with paged_key_kernel for long
+//            tables, paged_move_kernel)
 #include "common.h"
 #include "attend_wave.h"
 
